@@ -53,6 +53,7 @@ extern "C" {
 #define MOE_MAX_K 16
 #define MOE_MAX_E 1024
 #define MOE_MAX_DIM 262144
+#define MOE_MAX_GROUPS 65535
 #define MOE_LLEP_MAX_RANKS 64
 #define MOE_LLEP_MAX_GRANULE 65536
 #define MOE_PERMUTE_NOALLOC_MAX_BYTES 8388608
@@ -135,6 +136,59 @@ int moe_route_bwd(const moe_bf16* x, const float* w_router, const float* logits,
                   int64_t T, int d, int E, int k, int renorm, float* dw_router, float* dbias,
                   moe_bf16* dx, int dx_accumulate, float* dlogits, void* workspace,
                   size_t workspace_bytes, void* stream);
+
+/* moe_route_bwd_aux: moe_route_bwd with logit gradients of other losses of
+ * the router (moe_balance_loss_bwd's) added: dlogits_aux [T][E] fp32 joins
+ * each dlogits[t][e] by one fp32 add before the products.  Everything else,
+ * the workspace included, is moe_route_bwd's.
+ */
+int moe_route_bwd_aux(const moe_bf16* x, const float* w_router, const float* logits,
+                      const int32_t* topk_idx, const float* topk_gate, const float* dgate,
+                      const float* dlogits_aux, int64_t T, int d, int E, int k, int renorm,
+                      float* dw_router, float* dbias, moe_bf16* dx, int dx_accumulate,
+                      float* dlogits, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------ balance loss
+ * Balance loss, z-loss and per-expert counts of the router (the imbalance
+ * that Sec. 3.3 spreads over ranks is what these losses train away), over G
+ * groups of consecutive tokens: group g is tokens [seq_offsets[g],
+ * seq_offsets[g + 1]) (packed sequences, empty ones allowed), or, with
+ * seq_offsets = NULL and G = 1, all T tokens.  token_mask (optional): a token
+ * whose byte is 0 (padding) takes no part; its logits may hold anything.
+ * With p_t = softmax of logits[t] over all E, lse_t its log-sum-exp, and over
+ * the valid tokens t of group g:
+ *   n_tokens[g]    = how many there are
+ *   counts[g][e]   = slots (t, i) with topk_idx[t][i] = e
+ *   prob_sum[g][e] = sum over t of p_t[e]
+ *   balance[g] = E / (k n^2) sum over e of counts[g][e] prob_sum[g][e]
+ *   zloss[g]   = (1 / n) sum over t of lse_t^2
+ * (balance is 1 for equal loads and E / k at most; a group without valid
+ * tokens has 0).  Counts carry no gradient; given dbalance, dzloss [G] =
+ * dL/dbalance, dL/dzloss:
+ *   dlogits[t][e] = p_t[e] ( (dbalance / n) (a_e - sum over e' of a_e' p_t[e'])
+ *                            + (2 dzloss / n) lse_t ),  a_e = E counts[g][e] / (k n)
+ * and 0 for tokens masked out or in no group.  accumulate = 1 adds to dlogits
+ * instead, leaving those rows as they are.  The backward takes counts and
+ * n_tokens back: summed over data-parallel ranks first, both it and the loss
+ * formed from the summed counts, prob_sum and n_tokens are those of the whole
+ * batch.  Sums are fp32 in a fixed order.
+ *
+ * logits [T][E] fp32 (as moe_route wrote them); topk_idx [T][k] int32 (ids
+ * outside [0, E) are not counted); seq_offsets [G + 1] int32, ascending, in
+ * [0, T]; token_mask [T] bytes; balance, zloss [G] fp32; counts [G][E] int32;
+ * prob_sum [G][E] fp32; n_tokens [G] int32.  A row of -inf logits has p = 0
+ * and lse = 0; NaN and +inf logits of valid tokens make the group's sums NaN.
+ * Limits: 1 <= G <= MOE_MAX_GROUPS.  T = 0 is valid.
+ */
+int moe_balance_loss_workspace_bytes(int64_t T, int E, int G, size_t* bytes);
+int moe_balance_loss_fwd(const float* logits, const int32_t* topk_idx, const int32_t* seq_offsets,
+                         const uint8_t* token_mask, int64_t T, int E, int k, int G,
+                         float* balance, float* zloss, int32_t* counts, float* prob_sum,
+                         int32_t* n_tokens, void* workspace, size_t workspace_bytes, void* stream);
+int moe_balance_loss_bwd(const float* logits, const int32_t* counts, const int32_t* n_tokens,
+                         const float* dbalance, const float* dzloss, const int32_t* seq_offsets,
+                         const uint8_t* token_mask, int64_t T, int E, int k, int G, float* dlogits,
+                         int accumulate, void* stream);
 
 /* ------------------------------------------------------------- permutation
  * Group this device's token-expert assignments into contiguous per-expert

@@ -23,7 +23,8 @@ MOE_PERMUTE_NOALLOC_MAX_BYTES = 8 << 20
 C_SYMBOLS = (
     "moe_abi_version", "moe_status_string", "moe_last_error",
     "moe_route_workspace_bytes", "moe_route",
-    "moe_route_bwd_workspace_bytes", "moe_route_bwd",
+    "moe_route_bwd_workspace_bytes", "moe_route_bwd", "moe_route_bwd_aux",
+    "moe_balance_loss_workspace_bytes", "moe_balance_loss_fwd", "moe_balance_loss_bwd",
     "moe_permute_workspace_bytes", "moe_permute", "moe_permute_noalloc",
     "moe_grouped_swiglu_workspace_bytes", "moe_grouped_swiglu_fwd", "moe_grouped_swiglu_bwd",
     "moe_combine", "moe_combine_bwd",
@@ -59,6 +60,10 @@ def load(path: str = None):
         "moe_route": ([P, P, P, I64, I, I, I, I, P, P, P, P, SZ, P], I),
         "moe_route_bwd_workspace_bytes": ([I64, I, I, PSZ], I),
         "moe_route_bwd": ([P, P, P, P, P, P, I64, I, I, I, I, P, P, P, I, P, P, SZ, P], I),
+        "moe_route_bwd_aux": ([P, P, P, P, P, P, P, I64, I, I, I, I, P, P, P, I, P, P, SZ, P], I),
+        "moe_balance_loss_workspace_bytes": ([I64, I, I, PSZ], I),
+        "moe_balance_loss_fwd": ([P, P, P, P, I64, I, I, I, P, P, P, P, P, P, SZ, P], I),
+        "moe_balance_loss_bwd": ([P, P, P, P, P, P, P, I64, I, I, I, P, I, P], I),
         "moe_permute_workspace_bytes": ([I64, I, I, I, PSZ], I),
         "moe_permute": ([P, P, I64, I, I, I, I, I, P, P, P, P, P, P, SZ, P], I),
         "moe_permute_noalloc": ([P, P, I64, I, I, I, I, I, P, P, P, P, P, P], I),

@@ -89,7 +89,8 @@ const char* const kNames[moe::K_NUM] = {
     "gemm_fwd_down", "gemm_dgrad_down", "gemm_dgrad_gate_up", "gemm_wgrad_gate_up",
     "gemm_wgrad_down", "combine",       "combine_bwd",        "route_dlogits",
     "route_dw",     "route_dx",        "vocab_lse",          "vocab_grad",    "llep_plan",     "llep_window",
-    "route_split",  "vocab_logits",    "vocab_dx",           "vocab_dw"};
+    "route_split",  "vocab_logits",    "vocab_dx",           "vocab_dw",
+    "balance_part", "balance_sum",     "balance_bwd"};
 
 }  // namespace
 
@@ -186,12 +187,11 @@ MOE_API int moe_route_bwd_workspace_bytes(int64_t T, int d, int E, size_t* bytes
   return MOE_OK;
 }
 
-MOE_API int moe_route_bwd(const moe_bf16* x, const float* w_router, const float* logits,
-                          const int32_t* topk_idx, const float* topk_gate, const float* dgate,
-                          int64_t T, int d, int E, int k, int renorm, float* dw_router,
-                          float* dbias, moe_bf16* dx, int dx_accumulate, float* dlogits,
-                          void* workspace, size_t workspace_bytes, void* stream) {
-  const char* fn = "moe_route_bwd";
+static int route_bwd(const char* fn, const moe_bf16* x, const float* w_router, const float* logits,
+                     const int32_t* topk_idx, const float* topk_gate, const float* dgate,
+                     const float* dlogits_aux, int64_t T, int d, int E, int k, int renorm,
+                     float* dw_router, float* dbias, moe_bf16* dx, int dx_accumulate,
+                     float* dlogits, void* workspace, size_t workspace_bytes, void* stream) {
   if (int r = check_tk(fn, T, E, k)) return r;
   if (int r = check_dim(fn, d, "d")) return r;
   CHECK(renorm == 0 || renorm == 1, "renorm must be 0 or 1");
@@ -209,9 +209,90 @@ MOE_API int moe_route_bwd(const moe_bf16* x, const float* w_router, const float*
       return fail(MOE_ERR_WORKSPACE, fn, "workspace smaller than moe_route_bwd_workspace_bytes()");
     OPT(workspace);
   }
-  return hip_status(moe::launch_route_bwd(x, w_router, logits, topk_idx, topk_gate, dgate, T, d,
-                                          E, k, renorm, dw_router, dbias, dx, dx_accumulate,
-                                          dlogits, workspace, static_cast<hipStream_t>(stream)),
+  return hip_status(moe::launch_route_bwd(x, w_router, logits, topk_idx, topk_gate, dgate,
+                                          dlogits_aux, T, d, E, k, renorm, dw_router, dbias, dx,
+                                          dx_accumulate, dlogits, workspace,
+                                          static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+MOE_API int moe_route_bwd(const moe_bf16* x, const float* w_router, const float* logits,
+                          const int32_t* topk_idx, const float* topk_gate, const float* dgate,
+                          int64_t T, int d, int E, int k, int renorm, float* dw_router,
+                          float* dbias, moe_bf16* dx, int dx_accumulate, float* dlogits,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+  return route_bwd("moe_route_bwd", x, w_router, logits, topk_idx, topk_gate, dgate, nullptr, T, d,
+                   E, k, renorm, dw_router, dbias, dx, dx_accumulate, dlogits, workspace,
+                   workspace_bytes, stream);
+}
+
+MOE_API int moe_route_bwd_aux(const moe_bf16* x, const float* w_router, const float* logits,
+                              const int32_t* topk_idx, const float* topk_gate, const float* dgate,
+                              const float* dlogits_aux, int64_t T, int d, int E, int k, int renorm,
+                              float* dw_router, float* dbias, moe_bf16* dx, int dx_accumulate,
+                              float* dlogits, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  const char* fn = "moe_route_bwd_aux";
+  if (T > 0) REQ(dlogits_aux);
+  return route_bwd(fn, x, w_router, logits, topk_idx, topk_gate, dgate, dlogits_aux, T, d, E, k,
+                   renorm, dw_router, dbias, dx, dx_accumulate, dlogits, workspace,
+                   workspace_bytes, stream);
+}
+
+// ---------------------------------------------------------- balance loss
+static int check_balance(const char* fn, int64_t T, int E, int k, int G, const void* seq_offsets) {
+  if (int r = check_tk(fn, T, E, k)) return r;
+  CHECK(G >= 1 && G <= MOE_MAX_GROUPS, "G out of [1, MOE_MAX_GROUPS]");
+  CHECK(seq_offsets != nullptr || G == 1, "seq_offsets is NULL with G > 1");
+  OPT(seq_offsets);
+  return MOE_OK;
+}
+
+MOE_API int moe_balance_loss_workspace_bytes(int64_t T, int E, int G, size_t* bytes) {
+  const char* fn = "moe_balance_loss_workspace_bytes";
+  CHECK(bytes != nullptr, "bytes is NULL");
+  if (int r = check_tk(fn, T, E, 1)) return r;
+  CHECK(G >= 1 && G <= MOE_MAX_GROUPS, "G out of [1, MOE_MAX_GROUPS]");
+  *bytes = moe::balance_ws_bytes(T, E, G);
+  return MOE_OK;
+}
+
+MOE_API int moe_balance_loss_fwd(const float* logits, const int32_t* topk_idx,
+                                 const int32_t* seq_offsets, const uint8_t* token_mask, int64_t T,
+                                 int E, int k, int G, float* balance, float* zloss,
+                                 int32_t* counts, float* prob_sum, int32_t* n_tokens,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "moe_balance_loss_fwd";
+  if (int r = check_balance(fn, T, E, k, G, seq_offsets)) return r;
+  REQ(balance); REQ(zloss); REQ(counts); REQ(prob_sum); REQ(n_tokens);
+  if (T > 0) {
+    REQ(logits); REQ(topk_idx);
+    OPT(token_mask);
+  }
+  if (workspace == nullptr || workspace_bytes < moe::balance_ws_bytes(T, E, G))
+    return fail(MOE_ERR_WORKSPACE, fn, "workspace smaller than moe_balance_loss_workspace_bytes()");
+  OPT(workspace);
+  return hip_status(moe::launch_balance_fwd(logits, topk_idx, seq_offsets, token_mask, T, E, k, G,
+                                            balance, zloss, counts, prob_sum, n_tokens, workspace,
+                                            static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+MOE_API int moe_balance_loss_bwd(const float* logits, const int32_t* counts,
+                                 const int32_t* n_tokens, const float* dbalance,
+                                 const float* dzloss, const int32_t* seq_offsets,
+                                 const uint8_t* token_mask, int64_t T, int E, int k, int G,
+                                 float* dlogits, int accumulate, void* stream) {
+  const char* fn = "moe_balance_loss_bwd";
+  if (int r = check_balance(fn, T, E, k, G, seq_offsets)) return r;
+  CHECK(accumulate == 0 || accumulate == 1, "accumulate must be 0 or 1");
+  if (T > 0) {
+    REQ(logits); REQ(counts); REQ(n_tokens); REQ(dbalance); REQ(dzloss); REQ(dlogits);
+    OPT(token_mask);
+  }
+  return hip_status(moe::launch_balance_bwd(logits, seq_offsets, token_mask, counts, n_tokens,
+                                            dbalance, dzloss, T, E, k, G, accumulate, dlogits,
+                                            static_cast<hipStream_t>(stream)),
                     fn);
 }
 

@@ -91,6 +91,9 @@ enum KernelId {
   K_VOC_LOGITS,
   K_VOC_DX,
   K_VOC_DW,
+  K_BALANCE_PART,
+  K_BALANCE_SUM,
+  K_BALANCE_BWD,
   K_NUM
 };
 
@@ -114,9 +117,18 @@ int route_bwd_chunks(int64_t T, int d, int E);
 size_t route_bwd_ws_bytes(int64_t T, int d, int E);
 hipError_t launch_route_bwd(const uint16_t* x, const float* w, const float* logits,
                             const int32_t* idx, const float* gate, const float* dgate,
-                            int64_t T, int d, int E, int k, int renorm, float* dw, float* dbias,
-                            uint16_t* dx, int dx_accumulate, float* dlogits, void* ws,
-                            hipStream_t s);
+                            const float* aux, int64_t T, int d, int E, int k, int renorm,
+                            float* dw, float* dbias, uint16_t* dx, int dx_accumulate,
+                            float* dlogits, void* ws, hipStream_t s);
+size_t balance_ws_bytes(int64_t T, int E, int G);
+hipError_t launch_balance_fwd(const float* logits, const int32_t* idx, const int32_t* off,
+                              const uint8_t* mask, int64_t T, int E, int k, int G, float* balance,
+                              float* zloss, int32_t* counts, float* prob_sum, int32_t* n_tokens,
+                              void* ws, hipStream_t s);
+hipError_t launch_balance_bwd(const float* logits, const int32_t* off, const uint8_t* mask,
+                              const int32_t* counts, const int32_t* n_tokens,
+                              const float* dbalance, const float* dzloss, int64_t T, int E, int k,
+                              int G, int accumulate, float* dlogits, hipStream_t s);
 size_t vocab_fwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock);
 size_t vocab_bwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock);
 hipError_t launch_vocab_fwd(const uint16_t* x, const uint16_t* w, const int32_t* target,

@@ -27,12 +27,14 @@ namespace {
 //   renorm = 1 (gates = softmax over the k chosen logits):
 //     dl_{e_i} = gate_i (dgate_i - s), 0 for experts not chosen.
 // p_e is recomputed from the logits the forward pass saved, as the forward
-// computed it (max-shifted exponentials over all E).
+// computed it (max-shifted exponentials over all E).  aux (optional): logit
+// gradients of other losses of the router, added.
 template <int NV>
 __global__ __launch_bounds__(256) void route_dlogits_kernel(const float* __restrict__ logits,
                                                             const int32_t* __restrict__ idx,
                                                             const float* __restrict__ gate,
                                                             const float* __restrict__ dgate,
+                                                            const float* __restrict__ aux,
                                                             int64_t T, int E, int k, int renorm,
                                                             float* __restrict__ dl) {
   const int lane = threadIdx.x & 63;
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(256) void route_dlogits_kernel(const float* __restr
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int e = lane + 64 * j;
-    if (e < E) dl[t * E + e] = v[j];
+    if (e < E) dl[t * E + e] = aux != nullptr ? v[j] + aux[t * E + e] : v[j];
   }
 }
 
@@ -502,9 +504,9 @@ hipError_t launch_route_bwd_mfma(const uint16_t* x, const float* w, int64_t T, i
 
 hipError_t launch_route_bwd(const uint16_t* x, const float* w, const float* logits,
                             const int32_t* idx, const float* gate, const float* dgate,
-                            int64_t T, int d, int E, int k, int renorm, float* dw, float* dbias,
-                            uint16_t* dx, int dx_accumulate, float* dlogits, void* ws,
-                            hipStream_t s) {
+                            const float* aux, int64_t T, int d, int E, int k, int renorm,
+                            float* dw, float* dbias, uint16_t* dx, int dx_accumulate,
+                            float* dlogits, void* ws, hipStream_t s) {
   char* p = static_cast<char*>(ws);
   float* dl = dlogits;
   if (dl == nullptr) {
@@ -520,15 +522,16 @@ hipError_t launch_route_bwd(const uint16_t* x, const float* w, const float* logi
   const unsigned g1 = static_cast<unsigned>(ceil_div(T, 4));
   prof_begin(K_ROUTE_DLOGITS, s);
   if (E <= 64)
-    route_dlogits_kernel<1><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, T, E, k, renorm, dl);
+    route_dlogits_kernel<1><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, aux, T, E, k, renorm, dl);
   else if (E <= 128)
-    route_dlogits_kernel<2><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, T, E, k, renorm, dl);
+    route_dlogits_kernel<2><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, aux, T, E, k, renorm, dl);
   else if (E <= 256)
-    route_dlogits_kernel<4><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, T, E, k, renorm, dl);
+    route_dlogits_kernel<4><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, aux, T, E, k, renorm, dl);
   else if (E <= 512)
-    route_dlogits_kernel<8><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, T, E, k, renorm, dl);
+    route_dlogits_kernel<8><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, aux, T, E, k, renorm, dl);
   else
-    route_dlogits_kernel<16><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, T, E, k, renorm, dl);
+    route_dlogits_kernel<16><<<g1, 256, 0, s>>>(logits, idx, gate, dgate, aux, T, E, k, renorm,
+                                                dl);
   prof_end(K_ROUTE_DLOGITS, s);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;

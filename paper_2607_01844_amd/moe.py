@@ -64,6 +64,24 @@ def _need(t, dtype, name, dim=None):
     raise ValueError(f"{name}: expected {dim} dims, got {t.dim()}")
 
 
+def _given(t, dtype, name, shape):
+    """A tensor argument of exactly this type and shape on the current device
+    (kernels run on the current device's current stream)."""
+    _need(t, dtype, name, len(shape))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device")
+    return t
+
+
+def _out(t, dtype, name, shape, device):
+    """An output: the caller's tensor, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return _given(t, dtype, name, shape)
+
+
 _ws_cache: dict = {}
 _ws_retired: list = []
 
@@ -116,8 +134,10 @@ def moe_route(x, w_router, router_bias, k, renorm=0, logits=None, topk_idx=None,
 
 
 def moe_route_bwd(x, w_router, logits, topk_idx, topk_gate, dgate, renorm=0, dx=None,
-                  dx_accumulate=True, with_dbias=False, dlogits=None, dw_router=None):
-    """Router gradient from the gate gradients.
+                  dx_accumulate=True, with_dbias=False, dlogits=None, dw_router=None,
+                  dlogits_aux=None):
+    """Router gradient from the gate gradients, and from logit gradients of
+    other losses of the router (dlogits_aux [T,E] fp32, optional).
 
     Returns (dw_router [d,E] fp32, dbias [E] fp32 or None, dx or None).  When
     dx is given it is updated in place (dx_accumulate) or overwritten with the
@@ -143,11 +163,80 @@ def moe_route_bwd(x, w_router, logits, topk_idx, topk_gate, dgate, renorm=0, dx=
         _need(dw_router, torch.float32, "dw_router", 2)
     dbias = torch.empty((E,), dtype=torch.float32, device=dev) if with_dbias else None
     ws = workspace(_ws_bytes("moe_route_bwd_workspace_bytes", T, d, E), dev, "route_bwd")
-    _check(lib.moe_route_bwd(_ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx),
-                             _ptr(topk_gate), _ptr(dgate), T, d, E, k, renorm, _ptr(dw_router),
-                             _ptr(dbias), _ptr(dx), 1 if dx_accumulate else 0, _ptr(dlogits),
-                             _ptr(ws), ws.numel(), _stream()), "moe_route_bwd")
+    rest = (T, d, E, k, renorm, _ptr(dw_router), _ptr(dbias), _ptr(dx), 1 if dx_accumulate else 0,
+            _ptr(dlogits), _ptr(ws), ws.numel(), _stream())
+    if dlogits_aux is None:
+        _check(lib.moe_route_bwd(_ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx),
+                                 _ptr(topk_gate), _ptr(dgate), *rest), "moe_route_bwd")
+    else:
+        _given(dlogits_aux, torch.float32, "dlogits_aux", (T, E))
+        _check(lib.moe_route_bwd_aux(_ptr(x), _ptr(w_router), _ptr(logits), _ptr(topk_idx),
+                                     _ptr(topk_gate), _ptr(dgate), _ptr(dlogits_aux), *rest),
+               "moe_route_bwd_aux")
     return dw_router, dbias, dx
+
+
+# ---------------------------------------------------------- balance loss
+def _groups(logits, seq_offsets, token_mask):
+    """(T, E, G) of a balance loss call, its arguments checked."""
+    _need(logits, torch.float32, "logits", 2)
+    T, E = logits.shape
+    _given(logits, torch.float32, "logits", (T, E))
+    G = 1
+    if seq_offsets is not None:
+        _need(seq_offsets, torch.int32, "seq_offsets", 1)
+        G = seq_offsets.shape[0] - 1
+        if G < 1:
+            raise ValueError("seq_offsets needs two entries or more")
+        _given(seq_offsets, torch.int32, "seq_offsets", (G + 1,))
+    if token_mask is not None:
+        if token_mask.dtype not in (torch.bool, torch.uint8):
+            raise TypeError(f"token_mask: expected torch.bool or torch.uint8, got {token_mask.dtype}")
+        _given(token_mask, token_mask.dtype, "token_mask", (T,))
+    return T, E, G
+
+
+def moe_balance_loss_fwd(logits, topk_idx, seq_offsets=None, token_mask=None):
+    """Balance loss and z-loss of the router, per group of consecutive tokens
+    (seq_offsets [G+1] int32; None: one group).  logits [T,E] fp32, topk_idx
+    [T,k] int32, token_mask [T] bool or uint8 (0: padding).  Returns (balance
+    [G], zloss [G], counts [G,E] int32, prob_sum [G,E], n_tokens [G] int32)."""
+    T, E, G = _groups(logits, seq_offsets, token_mask)
+    _need(topk_idx, torch.int32, "topk_idx", 2)
+    k = topk_idx.shape[1]
+    _given(topk_idx, torch.int32, "topk_idx", (T, k))
+    dev = logits.device
+    balance = torch.empty((G,), dtype=torch.float32, device=dev)
+    zloss = torch.empty((G,), dtype=torch.float32, device=dev)
+    counts = torch.empty((G, E), dtype=torch.int32, device=dev)
+    prob_sum = torch.empty((G, E), dtype=torch.float32, device=dev)
+    n_tokens = torch.empty((G,), dtype=torch.int32, device=dev)
+    ws = workspace(_ws_bytes("moe_balance_loss_workspace_bytes", T, E, G), dev, "balance_loss")
+    _check(lib.moe_balance_loss_fwd(_ptr(logits), _ptr(topk_idx), _ptr(seq_offsets),
+                                    _ptr(token_mask), T, E, k, G, _ptr(balance), _ptr(zloss),
+                                    _ptr(counts), _ptr(prob_sum), _ptr(n_tokens), _ptr(ws),
+                                    ws.numel(), _stream()), "moe_balance_loss_fwd")
+    return balance, zloss, counts, prob_sum, n_tokens
+
+
+def moe_balance_loss_bwd(logits, counts, n_tokens, dbalance, dzloss, k, seq_offsets=None,
+                         token_mask=None, dlogits=None, accumulate=False):
+    """Gradient of the router's logits from dbalance, dzloss [G] fp32, with the
+    forward's counts and n_tokens (k: slots per token).  Returns dlogits [T,E]
+    fp32, overwritten, or added to where `accumulate`."""
+    T, E, G = _groups(logits, seq_offsets, token_mask)
+    _given(counts, torch.int32, "counts", (G, E))
+    _given(n_tokens, torch.int32, "n_tokens", (G,))
+    _given(dbalance, torch.float32, "dbalance", (G,))
+    _given(dzloss, torch.float32, "dzloss", (G,))
+    if accumulate and dlogits is None:
+        raise ValueError("accumulate needs dlogits")
+    dlogits = _out(dlogits, torch.float32, "dlogits", (T, E), logits.device)
+    _check(lib.moe_balance_loss_bwd(_ptr(logits), _ptr(counts), _ptr(n_tokens), _ptr(dbalance),
+                                    _ptr(dzloss), _ptr(seq_offsets), _ptr(token_mask), T, E, k, G,
+                                    _ptr(dlogits), 1 if accumulate else 0, _stream()),
+           "moe_balance_loss_bwd")
+    return dlogits
 
 
 # ------------------------------------------------------------ permutation
@@ -458,16 +547,25 @@ def profile_query() -> dict:
 
 # ------------------------------------------------------------- whole layer
 def layer_fwd_bwd(inp: dict, k: int, expert_begin=0, num_local=None, renorm=0,
-                  keep: bool = True) -> dict:
+                  keep: bool = True, router_loss=None) -> dict:
     """One forward + backward pass of the MoE expert layer through the C ABI.
 
     inp: x, w_router, router_bias, w_gate, w_up, w_down, dy (device tensors).
     Returns every intermediate (routing, permutation, activations, grads).
+
+    router_loss = (cb, cz) trains the router too: the step's loss also has cb
+    times the balance loss and cz times the z-loss of the whole batch (or, with
+    inp["seq_offsets"] and inp["token_mask"], their means over its sequences
+    and without its padding), dx becomes the whole layer's, and dw_router,
+    dbias (with a router bias), balance, zloss and expert_counts are returned.
     """
     x = inp["x"]
     E = inp["w_router"].shape[1]
     num_local = E if num_local is None else num_local
-    idx, gate = moe_route(x, inp["w_router"], inp.get("router_bias"), k, renorm)
+    logits = None
+    if router_loss is not None:
+        logits = torch.empty((x.shape[0], E), dtype=torch.float32, device=x.device)
+    idx, gate = moe_route(x, inp["w_router"], inp.get("router_bias"), k, renorm, logits=logits)
     pm = moe_permute(x, idx, E, expert_begin, num_local)
     off = pm["expert_offsets"]
     hg, hu, y_perm = moe_grouped_swiglu_fwd(pm["x_perm"], off, inp["w_gate"], inp["w_up"],
@@ -479,6 +577,19 @@ def layer_fwd_bwd(inp: dict, k: int, expert_begin=0, num_local=None, renorm=0,
     dx = moe_combine(dx_perm, pm["dst"], None)
     out = {"topk_idx": idx, "topk_gate": gate, "y": y, "dgate": dgate, "dx": dx,
            "dw_gate": dwg, "dw_up": dwu, "dw_down": dwd}
+    if router_loss is not None:
+        seq, mask = inp.get("seq_offsets"), inp.get("token_mask")
+        balance, zloss, counts, _, n = moe_balance_loss_fwd(logits, idx, seq, mask)
+        G = n.shape[0]
+        db, dz = (torch.full((G,), c / G, dtype=torch.float32, device=x.device)
+                  for c in router_loss)
+        aux = moe_balance_loss_bwd(logits, counts, n, db, dz, k, seq, mask)
+        dwr, dbias, _ = moe_route_bwd(x, inp["w_router"], logits, idx, gate, dgate, renorm, dx=dx,
+                                      with_dbias=inp.get("router_bias") is not None,
+                                      dlogits_aux=aux)
+        out.update(balance=balance, zloss=zloss, expert_counts=counts, dw_router=dwr)
+        if dbias is not None:
+            out["dbias"] = dbias
     if keep:
         out.update(pm)
         out.update(h_gate=hg, h_up=hu, y_perm=y_perm, dy_perm=dy_perm, dx_perm=dx_perm)
