@@ -54,6 +54,9 @@ extern "C" {
 #define MOE_MAX_E 1024
 #define MOE_MAX_DIM 262144
 #define MOE_MAX_GROUPS 65535
+#define MOE_DISTILL_MAX_K 256
+#define MOE_DISTILL_MIN_TEMPERATURE 0.0009765625f
+#define MOE_DISTILL_MAX_TEMPERATURE 1024.0f
 #define MOE_LLEP_MAX_RANKS 64
 #define MOE_LLEP_MAX_GRANULE 65536
 #define MOE_PERMUTE_NOALLOC_MAX_BYTES 8388608
@@ -398,6 +401,51 @@ int moe_vocab_loss_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* 
                        const float* lse, const float* dloss, int64_t N, int H, int64_t V,
                        int64_t vblock, moe_bf16* dx, moe_bf16* dw_voc, void* workspace,
                        size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------- distillation
+ * The same projection trained against a teacher's top logits instead of one
+ * target a row: Y = X W_voc, q_n = softmax over all V of Y[n] / tau, and a
+ * teacher of K slots a row, slot s naming vocabulary entry topk_idx[n][s]
+ * with logit topk_logit[n][s].  A slot whose entry is outside [0, V) (-1, say)
+ * is absent; several slots may name one entry (their probabilities add).
+ *   p_s = softmax over the present slots of topk_logit[n][s] / tau, or, with
+ *         teacher_lse, exp(topk_logit[n][s] / tau - teacher_lse[n]): the
+ *         teacher's own probability, its log-sum-exp (at tau) being over its
+ *         whole vocabulary (then sum_s p_s <= 1 is the share that the slots keep)
+ *   loss_n = sum_s p_s (log p_s - log q_n[topk_idx[n][s]])     (>= 0 where the
+ *         p_s sum to 1; a slot of p_s = 0 adds 0, a row without slots has 0)
+ * No factor tau^2 is applied (it belongs in dloss).  Blocks, limits and
+ * determinism are moe_vocab_loss's: the logits are never stored.
+ *
+ * x [N][H], w_voc [H][V] bf16; topk_idx [N][K] int32; topk_logit [N][K] fp32;
+ * teacher_lse [N] fp32 or NULL; the forward writes loss [N], lse [N] (log
+ * sum_v exp(Y[n][v] / tau)) and y_topk [N][K] fp32 (Y[n][topk_idx[n][s]]; 0 for
+ * absent slots), which the backward takes back.  Given dloss [N] = dL/dloss it
+ * recomputes each block of logits and writes dx [N][H] = G W_voc^T and
+ * dw_voc [H][V] = X^T G in bf16 (fp32 sums; zeros in dw_voc when N = 0) with
+ *   G[n][v] = dloss_n / tau ((sum_s p_s) q_n[v] - sum of p_s over slots of v)
+ * rounded to bf16 before the two products.  The teacher gets no gradient.
+ * Limits: those of moe_vocab_loss, N < 2^26, 1 <= K <= MOE_DISTILL_MAX_K,
+ * N * K < 2^31, tau within
+ * [MOE_DISTILL_MIN_TEMPERATURE, MOE_DISTILL_MAX_TEMPERATURE].  Present slots'
+ * logits are finite or -inf (p_s = 0); NaN and +inf make the row's results NaN.
+ * workspace: moe_vocab_distill_workspace_bytes() bytes (serves both calls:
+ * moe_vocab_loss's, the teacher's probabilities and entries, and a bit per row
+ * and 64 columns).
+ */
+int moe_vocab_distill_workspace_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K,
+                                      size_t* bytes);
+int moe_vocab_distill_fwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* topk_idx,
+                          const float* topk_logit, const float* teacher_lse, float temperature,
+                          int64_t N, int H, int64_t V, int64_t vblock, int K, float* loss,
+                          float* lse, float* y_topk, void* workspace, size_t workspace_bytes,
+                          void* stream);
+int moe_vocab_distill_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* topk_idx,
+                          const float* topk_logit, const float* teacher_lse, float temperature,
+                          const float* lse, const float* y_topk, const float* dloss, int64_t N,
+                          int H, int64_t V, int64_t vblock, int K, moe_bf16* dx,
+                          moe_bf16* dw_voc, void* workspace, size_t workspace_bytes,
+                          void* stream);
 
 /* ------------------------------------------ least-loaded expert parallelism
  * Sec. 3.3 (recap of LLEP): the load of each rank is taken at every call

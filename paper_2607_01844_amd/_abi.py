@@ -31,6 +31,7 @@ C_SYMBOLS = (
     "moe_ffn_fwd_chunked_workspace_bytes", "moe_ffn_fwd_chunked",
     "moe_ffn_fwd_row_chunked_workspace_bytes", "moe_ffn_fwd_row_chunked",
     "moe_vocab_loss_workspace_bytes", "moe_vocab_loss_fwd", "moe_vocab_loss_bwd",
+    "moe_vocab_distill_workspace_bytes", "moe_vocab_distill_fwd", "moe_vocab_distill_bwd",
     "moe_llep_plan", "moe_llep_dispatch",
     "moe_profile_enable", "moe_profile_reset", "moe_profile_num_kernels",
     "moe_profile_kernel_name", "moe_profile_query",
@@ -51,6 +52,7 @@ def load(path: str = None):
             "(there is no CPU fallback)")
     L = ctypes.CDLL(path)
     P, I, I64, U, SZ = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint, ctypes.c_size_t
+    F = ctypes.c_float
     PSZ = ctypes.POINTER(ctypes.c_size_t)
     sig = {
         "moe_abi_version": ([], I),
@@ -81,6 +83,10 @@ def load(path: str = None):
         "moe_vocab_loss_workspace_bytes": ([I64, I, I64, I64, PSZ], I),
         "moe_vocab_loss_fwd": ([P, P, P, I64, I, I64, I64, P, P, P, SZ, P], I),
         "moe_vocab_loss_bwd": ([P, P, P, P, P, I64, I, I64, I64, P, P, P, SZ, P], I),
+        "moe_vocab_distill_workspace_bytes": ([I64, I, I64, I64, I, PSZ], I),
+        "moe_vocab_distill_fwd": ([P, P, P, P, P, F, I64, I, I64, I64, I, P, P, P, P, SZ, P], I),
+        "moe_vocab_distill_bwd": ([P, P, P, P, P, F, P, P, P, I64, I, I64, I64, I, P, P, P, SZ, P],
+                                  I),
         "moe_llep_plan": ([P, I, I, I, I, P, P, P, P, P], I),
         "moe_llep_dispatch": ([P, P, P, P, P, P, I, I, I64, I, I, I, I64, P, P, P, P, P], I),
         "moe_profile_enable": ([I], I),

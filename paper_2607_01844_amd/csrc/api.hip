@@ -90,7 +90,7 @@ const char* const kNames[moe::K_NUM] = {
     "gemm_wgrad_down", "combine",       "combine_bwd",        "route_dlogits",
     "route_dw",     "route_dx",        "vocab_lse",          "vocab_grad",    "llep_plan",     "llep_window",
     "route_split",  "vocab_logits",    "vocab_dx",           "vocab_dw",
-    "balance_part", "balance_sum",     "balance_bwd"};
+    "balance_part", "balance_sum",     "balance_bwd",        "vocab_teacher"};
 
 }  // namespace
 
@@ -608,6 +608,73 @@ MOE_API int moe_vocab_loss_bwd(const moe_bf16* x, const moe_bf16* w_voc, const i
   }
   return hip_status(moe::launch_vocab_bwd(x, w_voc, target, lse, dloss, N, H, V, vblock, dx,
                                           dw_voc, workspace, static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+static int check_distill(const char* fn, int64_t N, int H, int64_t V, int64_t vblock, int K) {
+  if (int r = check_vocab(fn, N, H, V, vblock)) return r;
+  CHECK(K >= 1 && K <= MOE_DISTILL_MAX_K, "K out of [1, MOE_DISTILL_MAX_K]");
+  CHECK(N < (int64_t{1} << 26), "N out of [0, 2^26)");
+  CHECK(N * K < (int64_t{1} << 31), "N*K >= 2^31");
+  return MOE_OK;
+}
+
+MOE_API int moe_vocab_distill_workspace_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K,
+                                              size_t* bytes) {
+  const char* fn = "moe_vocab_distill_workspace_bytes";
+  CHECK(bytes != nullptr, "bytes is NULL");
+  if (int r = check_distill(fn, N, H, V, vblock, K)) return r;
+  *bytes = std::max(moe::distill_fwd_ws_bytes(N, H, V, vblock, K),
+                    moe::distill_bwd_ws_bytes(N, H, V, vblock, K));
+  return MOE_OK;
+}
+
+MOE_API int moe_vocab_distill_fwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* topk_idx,
+                                  const float* topk_logit, const float* teacher_lse,
+                                  float temperature, int64_t N, int H, int64_t V, int64_t vblock,
+                                  int K, float* loss, float* lse, float* y_topk, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  const char* fn = "moe_vocab_distill_fwd";
+  if (int r = check_distill(fn, N, H, V, vblock, K)) return r;
+  CHECK(temperature >= MOE_DISTILL_MIN_TEMPERATURE && temperature <= MOE_DISTILL_MAX_TEMPERATURE,
+        "temperature out of [MOE_DISTILL_MIN_TEMPERATURE, MOE_DISTILL_MAX_TEMPERATURE]");
+  if (N > 0) {
+    REQ(x); REQ(w_voc); REQ(topk_idx); REQ(topk_logit); REQ(loss); REQ(lse); REQ(y_topk);
+    OPT(teacher_lse);
+    if (workspace == nullptr || workspace_bytes < moe::distill_fwd_ws_bytes(N, H, V, vblock, K))
+      return fail(MOE_ERR_WORKSPACE, fn,
+                  "workspace smaller than moe_vocab_distill_workspace_bytes()");
+    OPT(workspace);
+  }
+  const moe::Teacher q{topk_idx, topk_logit, teacher_lse, K, temperature};
+  return hip_status(moe::launch_distill_fwd(x, w_voc, q, N, H, V, vblock, loss, lse, y_topk,
+                                            workspace, workspace_bytes,
+                                            static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+MOE_API int moe_vocab_distill_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* topk_idx,
+                                  const float* topk_logit, const float* teacher_lse,
+                                  float temperature, const float* lse, const float* y_topk,
+                                  const float* dloss, int64_t N, int H, int64_t V, int64_t vblock,
+                                  int K, moe_bf16* dx, moe_bf16* dw_voc, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  const char* fn = "moe_vocab_distill_bwd";
+  if (int r = check_distill(fn, N, H, V, vblock, K)) return r;
+  CHECK(temperature >= MOE_DISTILL_MIN_TEMPERATURE && temperature <= MOE_DISTILL_MAX_TEMPERATURE,
+        "temperature out of [MOE_DISTILL_MIN_TEMPERATURE, MOE_DISTILL_MAX_TEMPERATURE]");
+  REQ(dw_voc);
+  if (N > 0) {
+    REQ(x); REQ(w_voc); REQ(topk_idx); REQ(topk_logit); REQ(lse); REQ(y_topk); REQ(dloss); REQ(dx);
+    OPT(teacher_lse);
+    if (workspace == nullptr || workspace_bytes < moe::distill_bwd_ws_bytes(N, H, V, vblock, K))
+      return fail(MOE_ERR_WORKSPACE, fn,
+                  "workspace smaller than moe_vocab_distill_workspace_bytes()");
+    OPT(workspace);
+  }
+  const moe::Teacher q{topk_idx, topk_logit, teacher_lse, K, temperature};
+  return hip_status(moe::launch_distill_bwd(x, w_voc, q, lse, y_topk, dloss, N, H, V, vblock, dx,
+                                            dw_voc, workspace, static_cast<hipStream_t>(stream)),
                     fn);
 }
 

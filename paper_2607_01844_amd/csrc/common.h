@@ -94,6 +94,7 @@ enum KernelId {
   K_BALANCE_PART,
   K_BALANCE_SUM,
   K_BALANCE_BWD,
+  K_VOC_TEACHER,
   K_NUM
 };
 
@@ -137,6 +138,25 @@ hipError_t launch_vocab_fwd(const uint16_t* x, const uint16_t* w, const int32_t*
 hipError_t launch_vocab_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target,
                             const float* lse, const float* dloss, int64_t N, int H, int64_t V,
                             int64_t vblock, uint16_t* dx, uint16_t* dw, void* ws, hipStream_t s);
+// A teacher's top logits of every row: K slots ids, t [N][K] (an id outside
+// [0, V): no slot), tlse [N] its log-sum-exp or null (then the K slots'
+// probabilities sum to one).
+struct Teacher {
+  const int32_t* ids;
+  const float* t;
+  const float* tlse;
+  int K;
+  float tau;
+};
+size_t distill_fwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K);
+size_t distill_bwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K);
+hipError_t launch_distill_fwd(const uint16_t* x, const uint16_t* w, const Teacher& q, int64_t N,
+                              int H, int64_t V, int64_t vblock, float* loss, float* lse, float* yk,
+                              void* ws, size_t ws_bytes, hipStream_t s);
+hipError_t launch_distill_bwd(const uint16_t* x, const uint16_t* w, const Teacher& q,
+                              const float* lse, const float* yk, const float* dloss, int64_t N,
+                              int H, int64_t V, int64_t vblock, uint16_t* dx, uint16_t* dw,
+                              void* ws, hipStream_t s);
 size_t ffn_fwd_chunked_ws_bytes(int64_t chunk, int E, int k, int E_loc, int d, int f);
 size_t ffn_fwd_row_chunked_ws_bytes(int64_t T, int E, int k, int E_loc, int d, int f,
                                     int64_t chunk_rows);
@@ -210,6 +230,16 @@ hipError_t launch_vocab_grad_mfma(const uint16_t* x, const uint16_t* w, int64_t 
                                   int64_t v0, int N, int H, int vb, const int32_t* target,
                                   const float* lse, const float* dloss, uint16_t* G, int64_t gp,
                                   hipStream_t s);
+//   distill: the same pairs of y / tau, and yk[n][s] = y[n][ids[n][s]] for
+//     slots in the block (hits: see GemmArgs); G[n][c] = bf16(coef[n]
+//     exp(y / tau - lse[n])), zeros for c in [vb, gp).
+hipError_t launch_distill_logits_mfma(const uint16_t* x, const uint16_t* w, int64_t ldw,
+                                      int64_t bc0, int64_t v0, int N, int H, int vb, float it,
+                                      const uint32_t* hits, int hw, const int32_t* ids, int K,
+                                      int Kp, float* part, float* yk, hipStream_t s);
+hipError_t launch_distill_grad_mfma(const uint16_t* x, const uint16_t* w, int64_t ldw, int64_t bc0,
+                                    int N, int H, int vb, float it, const float* lse,
+                                    const float* coef, uint16_t* G, int64_t gp, hipStream_t s);
 hipError_t launch_vocab_dx_mfma(const uint16_t* G, int64_t gp, const uint16_t* w, int64_t ldw,
                                 int64_t bc0, int N, int H, int vb, int kspan, int first,
                                 float* dxa, hipStream_t s);

@@ -340,6 +340,29 @@ hipError_t launch_vocab_grad_mfma(const uint16_t* x, const uint16_t* w, int64_t 
   return run_dense<VOC_GRAD>(a, K_VOC_GRAD, s);
 }
 
+hipError_t launch_distill_logits_mfma(const uint16_t* x, const uint16_t* w, int64_t ldw,
+                                      int64_t bc0, int64_t v0, int N, int H, int vb, float it,
+                                      const uint32_t* hits, int hw, const int32_t* ids, int K,
+                                      int Kp, float* part, float* yk, hipStream_t s) {
+  GemmArgs a{};
+  a.da = x; a.db = w; a.dc = part; a.yk = yk;
+  a.a_ld = H; a.b_ld = ldw; a.bc0 = bc0; a.v0 = v0;
+  a.dM = N; a.dN = vb; a.dK = H; a.kspan = H; a.batches = 1;
+  a.it = it; a.hits = hits; a.hw = hw; a.ids = ids; a.K = K; a.Kp = Kp;
+  return run_dense<VD_FWD>(a, K_VOC_LOGITS, s);
+}
+
+hipError_t launch_distill_grad_mfma(const uint16_t* x, const uint16_t* w, int64_t ldw, int64_t bc0,
+                                    int N, int H, int vb, float it, const float* lse,
+                                    const float* coef, uint16_t* G, int64_t gp, hipStream_t s) {
+  GemmArgs a{};
+  a.da = x; a.db = w; a.dc = G; a.lse = lse; a.dloss = coef;
+  a.a_ld = H; a.b_ld = ldw; a.c_ld = gp; a.bc0 = bc0;
+  a.dM = N; a.dN = vb; a.dK = H; a.kspan = H; a.batches = 1;
+  a.it = it;
+  return run_dense<VD_GRAD>(a, K_VOC_GRAD, s);
+}
+
 hipError_t launch_vocab_dx_mfma(const uint16_t* G, int64_t gp, const uint16_t* w, int64_t ldw,
                                 int64_t bc0, int N, int H, int vb, int kspan, int first,
                                 float* dxa, hipStream_t s) {

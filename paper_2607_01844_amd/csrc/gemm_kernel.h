@@ -98,7 +98,9 @@ enum Mode {
   VOC_FWD,          // vocabulary: per row and 64 columns (max, sum exp), target logit
   VOC_GRAD,         // vocabulary: G = bf16(dl ([v == t] - exp(y - lse)))
   VOC_DX,           // vocabulary: dxa[b] (+)= G_b W_b^T, fp32
-  VOC_DW            // vocabulary: dW[:, block] = X^T G, bf16
+  VOC_DW,           // vocabulary: dW[:, block] = X^T G, bf16
+  VD_FWD,           // distillation: VOC_FWD of y / tau, and the logits at the teacher's slots
+  VD_GRAD           // distillation: G = bf16(c exp(y / tau - lse))
 };
 
 template <int MODE>
@@ -454,6 +456,12 @@ struct GemmArgs {
   int64_t cc0;              // vocabulary: dW's first column (VOC_DW)
   int dE;                   // router: experts (the lo parts sit 2E columns into DL3)
   int flag;                 // RT_DX: add to dx; VOC_DX: first block (store, no add)
+  // distillation (VD_FWD, VD_GRAD)
+  const uint32_t* hits;     // [N][hw]: bit g of a row: it has a slot in columns 64 g .. + 63
+  const int32_t* ids;       // [N][Kp]: vocabulary entry of each slot, -1: none
+  float* yk;                // [N][K]: logit at each slot
+  int hw, K, Kp;
+  float it;                 // 1 / tau
 };
 
 // Eight bf16 to an address of any alignment, the first n where n < 8 (the
@@ -1054,10 +1062,14 @@ __global__ __launch_bounds__(Geom<S>::NTHR, 2) void grouped_gemm_kernel(GemmArgs
             }
           });
         }
-      } else if constexpr (MODE == VOC_FWD) {
+      } else if constexpr (MODE == VOC_FWD || MODE == VD_FWD) {
         // Per row, the (max, sum of exp(y - max)) of this wave's 64 block
         // columns (lanes l and l + 32 hold 32 each), and the target's logit
-        // where this wave holds the target column.
+        // where this wave holds the target column.  Distillation: the pair of
+        // y / tau, and the logit of every slot of the teacher's that lies in
+        // the 64 columns.  Few rows have one (64 slots of 200,000 columns: one
+        // row in fifty), so a bit per row and 64 columns says where the row's
+        // slots are looked through at all.
         const int rt = rb + l32;
         const bool rok = rt < mvalid;
         const int64_t row = (int64_t)m0 + rt;
@@ -1072,13 +1084,17 @@ __global__ __launch_bounds__(Geom<S>::NTHR, 2) void grouped_gemm_kernel(GemmArgs
           });
         });
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        if constexpr (MODE == VD_FWD) mx *= g.it;
         float sm = 0.0f;
         if (mx != NEG) {
           static_for<2>([&](auto J) {
             static_for<16>([&](auto R) {
               constexpr int j = J, r = R;
               const int c = cb + 32 * j + 8 * (r / 4) + 4 * lh + (r % 4);
-              if (c < g.dN) sm += __expf(acc[i][j][r] - mx);
+              if (c < g.dN) {
+                if constexpr (MODE == VD_FWD) sm += __expf(__builtin_fmaf(acc[i][j][r], g.it, -mx));
+                else sm += __expf(acc[i][j][r] - mx);
+              }
             });
           });
         }
@@ -1087,19 +1103,48 @@ __global__ __launch_bounds__(Geom<S>::NTHR, 2) void grouped_gemm_kernel(GemmArgs
           const int ng = (g.dN + 63) >> 6;
           if (lh == 0 && cb < g.dN)
             reinterpret_cast<float2*>(g.dc)[row * ng + (cb >> 6)] = make_float2(mx, sm);
-          const int64_t tc = (int64_t)g.target[row] - g.v0 - cb;
-          if (tc >= 0 && tc < 64 && cb + tc < g.dN && ((tc >> 2) & 1) == lh) {
-            const int want = static_cast<int>(tc) & ~4;  // 32 j + 8 q + u
-            float val = 0.0f;
-            static_for<2>([&](auto J) {
-              static_for<16>([&](auto R) {
-                constexpr int j = J, r = R;
-                // a sum of selects (one term matches): the compiler keeps
-                // it in registers instead of indexing the accumulators
-                val += 32 * j + 8 * (r / 4) + (r % 4) == want ? acc[i][j][r] : 0.0f;
+          if constexpr (MODE == VOC_FWD) {
+            const int64_t tc = (int64_t)g.target[row] - g.v0 - cb;
+            if (tc >= 0 && tc < 64 && cb + tc < g.dN && ((tc >> 2) & 1) == lh) {
+              const int want = static_cast<int>(tc) & ~4;  // 32 j + 8 q + u
+              float val = 0.0f;
+              static_for<2>([&](auto J) {
+                static_for<16>([&](auto R) {
+                  constexpr int j = J, r = R;
+                  // a sum of selects (one term matches): the compiler keeps
+                  // it in registers instead of indexing the accumulators
+                  val += 32 * j + 8 * (r / 4) + (r % 4) == want ? acc[i][j][r] : 0.0f;
+                });
               });
-            });
-            g.yt[row] = val;
+              g.yt[row] = val;
+            }
+          }
+        }
+        if constexpr (MODE == VD_FWD) {
+          const bool in = rok && cb < g.dN;
+          const uint32_t word = in ? g.hits[row * g.hw + (cb >> 11)] : 0u;
+          const bool has = ((word >> ((cb >> 6) & 31)) & 1u) != 0;
+          if (__any(has)) {
+            const int first = static_cast<int>(g.v0) + cb;
+            for (int s = 0; s < g.Kp; s += 4) {
+              int4 q = make_int4(-1, -1, -1, -1);
+              if (has) q = *reinterpret_cast<const int4*>(g.ids + row * g.Kp + s);
+              const int id[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const int c = id[u] - first;
+                const bool hit = id[u] >= 0 && c >= 0 && c < 64 && cb + c < g.dN && ((c >> 2) & 1) == lh;
+                if (!__any(hit)) continue;
+                float val = 0.0f;
+                static_for<2>([&](auto J) {
+                  static_for<16>([&](auto R) {
+                    constexpr int j = J, r = R;
+                    val += 32 * j + 8 * (r / 4) + (r % 4) == (c & ~4) ? acc[i][j][r] : 0.0f;
+                  });
+                });
+                if (hit) g.yk[row * g.K + s + u] = val;
+              }
+            }
           }
         }
       } else if constexpr (MODE == RT_DX || MODE == VOC_DX) {
@@ -1186,6 +1231,24 @@ __global__ __launch_bounds__(Geom<S>::NTHR, 2) void grouped_gemm_kernel(GemmArgs
             });
           });
         }
+        if constexpr (MODE == VD_GRAD) {
+          // G = c exp(y / tau - lse) (0 where c is: a row without slots), 0
+          // past the block's columns; the slots' entries are set afterwards
+          const int rt = rb + l32;
+          float lse = 0.0f, cf = 0.0f;
+          if (rt < mvalid) {
+            lse = g.lse[(int64_t)m0 + rt];
+            cf = g.dloss[(int64_t)m0 + rt];
+          }
+          static_for<2>([&](auto J) {
+            static_for<16>([&](auto R) {
+              constexpr int j = J, r = R;
+              const int c = n0 + wn * 64 + 32 * j + 8 * (r / 4) + 4 * lh + (r % 4);
+              const float p = __expf(__builtin_fmaf(acc[i][j][r], g.it, -lse));
+              acc[i][j][r] = c < g.dN && cf != 0.0f ? cf * p : 0.0f;
+            });
+          });
+        }
         static_for<2>([&](auto J) {
           static_for<4>([&](auto Q) {
             constexpr int j = J, q = Q;
@@ -1202,13 +1265,14 @@ __global__ __launch_bounds__(Geom<S>::NTHR, 2) void grouped_gemm_kernel(GemmArgs
             const int rt = rb + r, col = n0 + wn * 64 + 8 * c;
             // column limit: d; the block's columns (VOC_DW); G's whole pitch,
             // zeros past the block included (VOC_GRAD)
-            const int climit = MODE == VOC_GRAD ? static_cast<int>(g.c_ld) : DENSE ? g.dN : d;
+            const int climit =
+                MODE == VOC_GRAD || MODE == VD_GRAD ? static_cast<int>(g.c_ld) : DENSE ? g.dN : d;
             if (rt < mvalid && col < climit) {
               uint16_t* out;
               if constexpr (MODE == FWD_DOWN) out = g.y + (int64_t)(seg + m0 + rt) * d;
               else if constexpr (MODE == DGRAD_GATE_UP) out = g.dx + (int64_t)(seg + m0 + rt) * d;
               else if constexpr (MODE == WGRAD_DOWN) out = g.dwd + e * wdf + (int64_t)(m0 + rt) * d;
-              else if constexpr (MODE == VOC_GRAD) out = static_cast<uint16_t*>(g.dc) + (int64_t)(m0 + rt) * g.c_ld;
+              else if constexpr (MODE == VOC_GRAD || MODE == VD_GRAD) out = static_cast<uint16_t*>(g.dc) + (int64_t)(m0 + rt) * g.c_ld;
               else out = static_cast<uint16_t*>(g.dc) + (int64_t)(m0 + rt) * g.c_ld + g.cc0;  // VOC_DW
               if constexpr (MODE == VOC_DW) store_any(out + col, v, g.dN - col);
               else if constexpr (MODE == FWD_DOWN || MODE == DGRAD_GATE_UP) store_perm<WHOLE>(out + col, v);

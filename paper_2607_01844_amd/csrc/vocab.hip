@@ -22,12 +22,27 @@
 // place of rows so long that a tile's rows lie further apart than a buffer
 // descriptor reaches (beyond 34 million columns in the forward, 4 million in
 // the backward), and blocks longer than that are cut (reach, below).
+//
+// Distillation from a teacher's top logits is the same walk with y / tau in
+// place of y: the forward's epilogue also picks up the student's logits at the
+// teacher's slots, and the backward's is G = dl / tau P exp(y / tau - lse), the
+// teacher's probabilities being subtracted at its slots (a few of every
+// thousand columns) by a small kernel before the two products.
 #include "common.h"
 
 #include <algorithm>
 
 namespace moe {
 namespace {
+
+// What the forward of distillation keeps of a teacher: the probability of each
+// slot [N][K] and the sum of p log p of each row.
+struct DistRows {
+  const float* p;
+  const float* plogp;
+  int K;
+  float it;  // 1 / tau
+};
 
 // Merge of two (max, sum of exp(y - max)) pairs; an empty pair is (-inf, 0).
 // The fused add is written out, so that every caller rounds alike.
@@ -53,14 +68,15 @@ __device__ __forceinline__ void lse_merge(float& m, float& s, float m2, float s2
 // loss and gradients: 497 us against 500 with one wave a row, and 499 with the
 // results in a launch of their own; forward of N = 2048, H = 64, V = 8192 in
 // blocks of 512: 20 us, with sub = 64 27, with sub = 8 but four waves 22).
-template <int W>
+// DIST (distillation): loss_n = sum_s p_s log p_s + sum_s p_s (lse_n - y_{n, s} / tau).
+template <int W, bool DIST>
 __global__ __launch_bounds__(256) void voc_merge_kernel(const float2* __restrict__ part, int ng,
                                                         int per, int sub, int64_t N,
                                                         float* __restrict__ m,
                                                         float* __restrict__ s, int first, int last,
                                                         const float* __restrict__ yt,
                                                         float* __restrict__ loss,
-                                                        float* __restrict__ lse) {
+                                                        float* __restrict__ lse, DistRows q) {
   constexpr int U = W == 1 ? 1 : 2;
   __shared__ float2 blk[W == 1 ? 1 : 64 * U * W];  // a block's pair each
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wv = wave % W;
@@ -125,6 +141,23 @@ __global__ __launch_bounds__(256) void voc_merge_kernel(const float2* __restrict
       __syncthreads();
     }
   }
+  if constexpr (DIST) {
+    if (last) {
+      if (wv != 0) return;
+      const float l = rm + logf(rs);
+      float a = 0.0f;
+      for (int j = lane; j < q.K; j += 64) {
+        const float p = q.p[n * q.K + j];
+        if (p != 0.0f) a = __builtin_fmaf(p, l - yt[n * q.K + j] * q.it, a);
+      }
+      a = wave_sum(a);
+      if (lane == 0) {
+        lse[n] = l;
+        loss[n] = q.plogp[n] + a;
+      }
+      return;
+    }
+  }
   if (lane == 0 && wv == 0) {
     if (last) {
       const float l = rm + logf(rs);
@@ -135,6 +168,151 @@ __global__ __launch_bounds__(256) void voc_merge_kernel(const float2* __restrict
       s[n] = rs;
     }
   }
+}
+
+// The teacher's probabilities of one row over a wave: lane l holds slots l, l +
+// 64, ...  p = 0 where a slot is absent (or its logit -inf); returns their sum,
+// and the sum of p log p.
+constexpr int DK = MOE_DISTILL_MAX_K / 64;
+__device__ __forceinline__ void teacher_row(const Teacher& q, float it, int64_t n, int64_t V, int lane,
+                                            int (&id)[DK], float (&p)[DK], float& P, float& plogp) {
+  constexpr float NEG = -__builtin_huge_valf();
+  float m = NEG;
+#pragma unroll
+  for (int i = 0; i < DK; ++i) {
+    const int j = lane + 64 * i;
+    id[i] = j < q.K ? q.ids[n * q.K + j] : -1;
+    if (id[i] >= V) id[i] = -1;
+    p[i] = id[i] >= 0 ? q.t[n * q.K + j] * it : NEG;
+    m = fmaxf(m, p[i]);
+  }
+  float shift;
+  if (q.tlse != nullptr) {
+    shift = q.tlse[n];
+  } else {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    const float mm = m == NEG ? 0.0f : m;
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < DK; ++i) s += id[i] >= 0 ? expf(p[i] - mm) : 0.0f;
+    s = wave_sum(s);
+    shift = s == 0.0f ? 0.0f : mm + logf(s);  // s = 0: every p below is 0
+  }
+  float a = 0.0f, b = 0.0f;
+#pragma unroll
+  for (int i = 0; i < DK; ++i) {
+    const float lp = p[i] - shift;
+    p[i] = id[i] >= 0 && p[i] != NEG ? expf(lp) : 0.0f;
+    a += p[i];
+    if (p[i] != 0.0f) b = __builtin_fmaf(p[i], lp, b);
+  }
+  P = wave_sum(a);
+  plogp = wave_sum(b);
+}
+
+// Forward, before the product over columns [b0, b0 + vb): one wave per row.
+// first: the teacher's probabilities, their p log p, the slots' ids with -1 for
+// absent ones (rows of Kp), and zeros for the absent ones' logits.  Then the
+// row's bits, one per 64 of the columns, set where a slot lies in them.
+constexpr int DW = 512;  // words of bits in LDS at a time
+__global__ __launch_bounds__(256) void distill_prep_kernel(Teacher q, float it, int64_t N, int64_t V,
+                                                           int64_t b0, int vb, int hw, int Kp,
+                                                           int first, float* __restrict__ p_out,
+                                                           float* __restrict__ plogp_out,
+                                                           int32_t* __restrict__ ids_out,
+                                                           float* __restrict__ yk,
+                                                           uint32_t* __restrict__ hits) {
+  __shared__ uint32_t bits[4][DW];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t n = static_cast<int64_t>(blockIdx.x) * 4 + w;
+  int id[DK];
+#pragma unroll
+  for (int i = 0; i < DK; ++i) id[i] = -1;
+  if (n < N) {
+    if (first) {
+      float p[DK], P, plogp;
+      teacher_row(q, it, n, V, lane, id, p, P, plogp);
+#pragma unroll
+      for (int i = 0; i < DK; ++i) {
+        const int j = lane + 64 * i;
+        if (j < q.K) {
+          p_out[n * q.K + j] = p[i];
+          if (id[i] < 0) yk[n * q.K + j] = 0.0f;
+        }
+        if (j < Kp) ids_out[n * Kp + j] = id[i];
+      }
+      if (lane == 0) plogp_out[n] = plogp;
+    } else {
+#pragma unroll
+      for (int i = 0; i < DK; ++i)
+        if (lane + 64 * i < Kp) id[i] = ids_out[n * Kp + lane + 64 * i];
+    }
+  }
+  for (int w0 = 0; w0 < hw; w0 += DW) {
+    const int nw = hw - w0 < DW ? hw - w0 : DW;
+    for (int i = lane; i < nw; i += 64) bits[w][i] = 0u;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < DK; ++i) {
+      const int64_t c = id[i] - b0;
+      const int64_t g = c >> 6, word = (g >> 5) - w0;
+      if (id[i] >= 0 && c >= 0 && c < vb && word >= 0 && word < nw)
+        atomicOr(&bits[w][word], 1u << (g & 31));
+    }
+    __syncthreads();
+    if (n < N)
+      for (int i = lane; i < nw; i += 64) hits[n * hw + w0 + i] = bits[w][i];
+    __syncthreads();
+  }
+}
+
+// Backward, once: coef_n = dl_n P_n / tau and dl_n p_s / tau of every slot.
+__global__ __launch_bounds__(256) void distill_coef_kernel(Teacher q, float it, int64_t N, int64_t V,
+                                                           const float* __restrict__ dloss,
+                                                           float* __restrict__ coef,
+                                                           float* __restrict__ dp) {
+  const int lane = threadIdx.x & 63;
+  const int64_t n = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (n >= N) return;
+  int id[DK];
+  float p[DK], P, plogp;
+  teacher_row(q, it, n, V, lane, id, p, P, plogp);
+  const float dl = dloss[n] * it;
+  if (lane == 0) coef[n] = dl * P;
+#pragma unroll
+  for (int i = 0; i < DK; ++i) {
+    const int j = lane + 64 * i;
+    if (j < q.K) dp[n * q.K + j] = dl * p[i];
+  }
+}
+
+// Backward, per block: G at the slots in its columns, from the forward's logits
+// there: G = coef exp(y / tau - lse) - sum of dl p / tau over the row's slots of
+// that column, one rounding.  Thread = slot; of slots of one column the first
+// writes.
+__global__ __launch_bounds__(256) void distill_slots_kernel(Teacher q, float it, int64_t N,
+                                                            int64_t b0, int vb,
+                                                            const float* __restrict__ coef,
+                                                            const float* __restrict__ dp,
+                                                            const float* __restrict__ yk,
+                                                            const float* __restrict__ lse,
+                                                            uint16_t* __restrict__ G, int64_t gp) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= N * q.K) return;
+  const int id = q.ids[i];
+  if (id < b0 || id - b0 >= vb) return;
+  const int64_t n = i / q.K;
+  const int j = static_cast<int>(i - n * q.K);
+  const int32_t* row = q.ids + n * q.K;
+  for (int s = 0; s < j; ++s)
+    if (row[s] == id) return;
+  float a = dp[i];
+  for (int s = j + 1; s < q.K; ++s)
+    if (row[s] == id) a += dp[n * q.K + s];
+  const float c = coef[n];
+  const float v = c != 0.0f ? __builtin_fmaf(c, __expf(__builtin_fmaf(yk[i], it, -lse[n])), -a) : -a;
+  G[n * gp + (id - b0)] = static_cast<uint16_t>(f32_to_bf16_bits(v));
 }
 
 // dx[i] = bf16(sum over slabs b ascending of dxa[b][i]), 8 values per thread
@@ -245,47 +423,25 @@ int64_t dx_kspan(int64_t N, int H, int64_t vblock) {
 }  // namespace
 
 namespace {
-size_t fwd_bytes(int64_t N, int H, int64_t V, int64_t span);
-// Columns the forward takes at once: the largest multiple of vblock whose
-// partial pairs (and staged copy of W) fit the workspace that
-// moe_vocab_loss_workspace_bytes() asks for, which the backward's buffers
-// set.  One product of many tiles instead of one per block: fewer launches
-// and partly filled last rounds (N = 1000, H = 520, V = 32003 in blocks of
-// 4096: 8 products and merges become 2; N = 4096, H = 2048, V = 200000: 13
-// become 1).  Blocks of fewer than 64 columns stay alone.  A copy of W stays
-// within reach and one launch (2^31 threads of eight columns).
-int64_t fwd_span(int64_t N, int H, int64_t V, int64_t vblock) {
-  const size_t room = std::max(vocab_fwd_ws_bytes(N, H, V, vblock), vocab_bwd_ws_bytes(N, H, V, vblock));
-  vblock = fwd_step(H, V, vblock);
-  if (vblock % 64 != 0) return vblock;
-  int64_t most = std::min<int64_t>(ceil_div(V, vblock), ((int64_t{1} << 40) - 1) / (N * vblock));
-  if (staged_fwd(H, V))
-    most = std::min(most, std::min(max_pitch(std::min(H, 32)), (int64_t{1} << 34) / H) / vblock);
-  int64_t lo = 1, hi = std::max<int64_t>(1, most);  // the largest m in [lo, hi] that fits
-  while (lo < hi) {
-    const int64_t mid = (lo + hi + 1) / 2;
-    if (fwd_bytes(N, H, V, mid * vblock) <= room) lo = mid; else hi = mid - 1;
-  }
-  return lo * vblock;
-}
-}  // namespace
+// Words of 32 bits that a row's columns take, one bit per 64 of them.
+int hit_words(int64_t vb) { return static_cast<int>(ceil_div(ceil_div(vb, 64), 32)); }
+int padded_slots(int K) { return static_cast<int>(align_up(static_cast<size_t>(K), 4)); }
 
-size_t vocab_fwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock) {
-  return fwd_bytes(N, H, V, fwd_block(H, V, vblock));
-}
-
-namespace {
-size_t fwd_bytes(int64_t N, int H, int64_t V, int64_t span) {
+// Workspace of a forward that takes `span` columns at once; K slots of a
+// teacher per row (0: the plain loss).
+size_t fwd_bytes(int64_t N, int H, int64_t V, int64_t span, int K) {
   const int64_t vb = std::min(span, V);
-  size_t b = align_up(sizeof(float) * 2 * static_cast<size_t>(N) * ceil_div(vb, 64), 256);  // pairs
-  b += 3 * align_up(sizeof(float) * static_cast<size_t>(N), 256);  // running max, sum; target logit
+  const size_t n = static_cast<size_t>(N);
+  size_t b = align_up(sizeof(float) * 2 * n * ceil_div(vb, 64), 256);  // pairs
+  b += 3 * align_up(sizeof(float) * n, 256);  // running max, sum; target logit (sum of p log p)
+  if (K > 0)
+    b += align_up(sizeof(float) * n * K, 256) + align_up(sizeof(int32_t) * n * padded_slots(K), 256) +
+         align_up(sizeof(uint32_t) * n * hit_words(vb), 256);
   if (staged_fwd(H, V))
     b += align_up(sizeof(uint16_t) * static_cast<size_t>(H) * align_up(vb, 8), 256);
   return b + 256;
 }
-}  // namespace
-
-size_t vocab_bwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock) {
+size_t bwd_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K) {
   vblock = bwd_block(N, H, V, vblock);
   const int64_t vb = std::min(vblock, V);
   const int64_t vbp = align_up(vb, 8);
@@ -294,16 +450,61 @@ size_t vocab_bwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock) {
   b += align_up(sizeof(float) * static_cast<size_t>(slabs) * N * H, 256);                // dX slabs
   if (staged_bwd(H, V, vblock))
     b += align_up(sizeof(uint16_t) * static_cast<size_t>(H) * vbp, 256);  // W
+  if (K > 0)
+    b += align_up(sizeof(float) * static_cast<size_t>(N), 256) +
+         align_up(sizeof(float) * static_cast<size_t>(N) * K, 256);  // coef, dl p
   return b + 256;
 }
+size_t fwd_least(int64_t N, int H, int64_t V, int64_t vblock, int K) {
+  return fwd_bytes(N, H, V, fwd_block(H, V, vblock), K);
+}
+// Columns the forward takes at once: the largest multiple of vblock whose
+// partial pairs (and staged copy of W) fit the workspace that
+// moe_vocab_loss_workspace_bytes() asks for, which the backward's buffers
+// set.  One product of many tiles instead of one per block: fewer launches
+// and partly filled last rounds (N = 1000, H = 520, V = 32003 in blocks of
+// 4096: 8 products and merges become 2; N = 4096, H = 2048, V = 200000: 13
+// become 1).  Blocks of fewer than 64 columns stay alone.  A copy of W stays
+// within reach and one launch (2^31 threads of eight columns).
+int64_t fwd_span(int64_t N, int H, int64_t V, int64_t vblock, int K) {
+  const size_t room = std::max(fwd_least(N, H, V, vblock, K), bwd_bytes(N, H, V, vblock, K));
+  vblock = fwd_step(H, V, vblock);
+  if (vblock % 64 != 0) return vblock;
+  int64_t most = std::min<int64_t>(ceil_div(V, vblock), ((int64_t{1} << 40) - 1) / (N * vblock));
+  if (staged_fwd(H, V))
+    most = std::min(most, std::min(max_pitch(std::min(H, 32)), (int64_t{1} << 34) / H) / vblock);
+  int64_t lo = 1, hi = std::max<int64_t>(1, most);  // the largest m in [lo, hi] that fits
+  while (lo < hi) {
+    const int64_t mid = (lo + hi + 1) / 2;
+    if (fwd_bytes(N, H, V, mid * vblock, K) <= room) lo = mid; else hi = mid - 1;
+  }
+  return lo * vblock;
+}
+}  // namespace
 
-hipError_t launch_vocab_fwd(const uint16_t* x, const uint16_t* w, const int32_t* target,
-                            int64_t N, int H, int64_t V, int64_t vblock, float* loss, float* lse,
-                            void* ws, size_t ws_bytes, hipStream_t s) {
+size_t vocab_fwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock) {
+  return fwd_least(N, H, V, vblock, 0);
+}
+size_t vocab_bwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock) {
+  return bwd_bytes(N, H, V, vblock, 0);
+}
+size_t distill_fwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K) {
+  return fwd_least(N, H, V, vblock, K);
+}
+size_t distill_bwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K) {
+  return bwd_bytes(N, H, V, vblock, K);
+}
+
+namespace {
+// The forward of either loss: against targets, or a teacher (q, yk).
+hipError_t run_fwd(const uint16_t* x, const uint16_t* w, const int32_t* target, const Teacher* q,
+                   int64_t N, int H, int64_t V, int64_t vblock, float* loss, float* lse, float* yk,
+                   void* ws, size_t ws_bytes, hipStream_t s) {
   if (N == 0) return hipSuccess;
+  const int K = q != nullptr ? q->K : 0;
   // a caller with room for the forward alone gets its blocks one by one
-  const int64_t span = ws_bytes >= vocab_bwd_ws_bytes(N, H, V, vblock) ? fwd_span(N, H, V, vblock)
-                                                                         : fwd_step(H, V, vblock);
+  const int64_t span = ws_bytes >= bwd_bytes(N, H, V, vblock, K) ? fwd_span(N, H, V, vblock, K)
+                                                                 : fwd_step(H, V, vblock);
   const int64_t vbmax = std::min(span, V);
   // groups of 64 columns per block
   const int per = static_cast<int>(ceil_div(std::min(fwd_step(H, V, vblock), V), 64));
@@ -318,6 +519,20 @@ hipError_t launch_vocab_fwd(const uint16_t* x, const uint16_t* w, const int32_t*
   p += align_up(sizeof(float) * static_cast<size_t>(N), 256);
   float* yt = reinterpret_cast<float*>(p);
   p += align_up(sizeof(float) * static_cast<size_t>(N), 256);
+  DistRows rows{};
+  float* prob = nullptr;
+  int32_t* ids = nullptr;
+  uint32_t* hits = nullptr;
+  const int Kp = padded_slots(K);
+  if (K > 0) {
+    prob = reinterpret_cast<float*>(p);
+    p += align_up(sizeof(float) * static_cast<size_t>(N) * K, 256);
+    ids = reinterpret_cast<int32_t*>(p);
+    p += align_up(sizeof(int32_t) * static_cast<size_t>(N) * Kp, 256);
+    hits = reinterpret_cast<uint32_t*>(p);
+    p += align_up(sizeof(uint32_t) * static_cast<size_t>(N) * hit_words(vbmax), 256);
+    rows = DistRows{prob, yt, K, 1.0f / q->tau};
+  }
   uint16_t* wst = staged_fwd(H, V) ? reinterpret_cast<uint16_t*>(p) : nullptr;
   const int n = static_cast<int>(N);
   for (int64_t b0 = 0; b0 < V; b0 += span) {
@@ -331,29 +546,47 @@ hipError_t launch_vocab_fwd(const uint16_t* x, const uint16_t* w, const int32_t*
       ldw = vbp;
       bc0 = 0;
     }
-    if (hipError_t e = launch_vocab_logits_mfma(x, wb, ldw, bc0, b0, n, H, vb, target, part, yt, s);
-        e != hipSuccess)
+    const int first = b0 == 0, last = b0 + span >= V;
+    if (K > 0) {
+      const int hw = hit_words(vb);
+      prof_begin(K_VOC_TEACHER, s);
+      distill_prep_kernel<<<static_cast<unsigned>(ceil_div(N, 4)), 256, 0, s>>>(
+          *q, rows.it, N, V, b0, vb, hw, Kp, first, prob, yt, ids, yk, hits);
+      prof_end(K_VOC_TEACHER, s);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+      if (hipError_t e = launch_distill_logits_mfma(x, wb, ldw, bc0, b0, n, H, vb, rows.it, hits, hw,
+                                                    ids, K, Kp, part, yk, s);
+          e != hipSuccess)
+        return e;
+    } else if (hipError_t e =
+                   launch_vocab_logits_mfma(x, wb, ldw, bc0, b0, n, H, vb, target, part, yt, s);
+               e != hipSuccess) {
       return e;
+    }
     prof_begin(K_VOC_LSE, s);
     const int ng = static_cast<int>(ceil_div(vb, 64));
     const float2* pairs = reinterpret_cast<const float2*>(part);
-    const int first = b0 == 0, last = b0 + span >= V;
     const int64_t rounds = ceil_div(ceil_div(ng, per), 64 / sub);  // of one wave a row
-    if (rounds <= (sub < 64 ? 4 : 1) || N > (int64_t{1} << 23))  // or rows enough
-      voc_merge_kernel<1><<<static_cast<unsigned>(ceil_div(N, 4)), 256, 0, s>>>(
-          pairs, ng, per, sub, N, m, sm, first, last, yt, loss, lse);
-    else
-      voc_merge_kernel<4><<<static_cast<unsigned>(N), 256, 0, s>>>(pairs, ng, per, sub, N, m, sm,
-                                                                   first, last, yt, loss, lse);
+    auto merge = [&](auto DIST) {
+      const float* at = DIST ? yk : yt;
+      if (rounds <= (sub < 64 ? 4 : 1) || N > (int64_t{1} << 23))  // or rows enough
+        voc_merge_kernel<1, DIST><<<static_cast<unsigned>(ceil_div(N, 4)), 256, 0, s>>>(
+            pairs, ng, per, sub, N, m, sm, first, last, at, loss, lse, rows);
+      else
+        voc_merge_kernel<4, DIST><<<static_cast<unsigned>(N), 256, 0, s>>>(
+            pairs, ng, per, sub, N, m, sm, first, last, at, loss, lse, rows);
+    };
+    if (K > 0) merge(std::true_type{});
+    else merge(std::false_type{});
     prof_end(K_VOC_LSE, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-hipError_t launch_vocab_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target,
-                            const float* lse, const float* dloss, int64_t N, int H, int64_t V,
-                            int64_t vblock, uint16_t* dx, uint16_t* dw, void* ws, hipStream_t s) {
+hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, const Teacher* q,
+                   const float* lse, const float* yk, const float* dloss, int64_t N, int H,
+                   int64_t V, int64_t vblock, uint16_t* dx, uint16_t* dw, void* ws, hipStream_t s) {
   if (N == 0) {  // no tokens: the weight gradient is exact zeros (dx is empty)
     const int64_t nw = static_cast<int64_t>(H) * V;
     voc_zero_bf16_kernel<<<static_cast<unsigned>(ceil_div(nw, 256)), 256, 0, s>>>(dw, nw);
@@ -371,7 +604,23 @@ hipError_t launch_vocab_bwd(const uint16_t* x, const uint16_t* w, const int32_t*
   p += align_up(sizeof(uint16_t) * static_cast<size_t>(N) * vbpmax, 256);
   float* dxa = reinterpret_cast<float*>(p);
   p += align_up(sizeof(float) * static_cast<size_t>(slabs) * N * H, 256);
-  uint16_t* wst = staged_bwd(H, V, vblock) ? reinterpret_cast<uint16_t*>(p) : nullptr;
+  uint16_t* wst = nullptr;
+  if (staged_bwd(H, V, vblock)) {
+    wst = reinterpret_cast<uint16_t*>(p);
+    p += align_up(sizeof(uint16_t) * static_cast<size_t>(H) * vbpmax, 256);
+  }
+  float *coef = nullptr, *dp = nullptr;
+  const float it = q != nullptr ? 1.0f / q->tau : 1.0f;
+  if (q != nullptr) {
+    coef = reinterpret_cast<float*>(p);
+    p += align_up(sizeof(float) * static_cast<size_t>(N), 256);
+    dp = reinterpret_cast<float*>(p);
+    prof_begin(K_VOC_TEACHER, s);
+    distill_coef_kernel<<<static_cast<unsigned>(ceil_div(N, 4)), 256, 0, s>>>(*q, it, N, V, dloss,
+                                                                              coef, dp);
+    prof_end(K_VOC_TEACHER, s);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
   const int n = static_cast<int>(N);
   for (int64_t b0 = 0; b0 < V; b0 += vblock) {
     const int vb = static_cast<int>(std::min<int64_t>(vblock, V - b0));
@@ -385,10 +634,20 @@ hipError_t launch_vocab_bwd(const uint16_t* x, const uint16_t* w, const int32_t*
       ldw = gp;
       bc0 = 0;
     }
-    if (hipError_t e = launch_vocab_grad_mfma(x, wb, ldw, bc0, b0, n, H, vb, target, lse, dloss, G,
-                                              gp, s);
-        e != hipSuccess)
+    if (q != nullptr) {
+      if (hipError_t e = launch_distill_grad_mfma(x, wb, ldw, bc0, n, H, vb, it, lse, coef, G, gp, s);
+          e != hipSuccess)
+        return e;
+      prof_begin(K_VOC_TEACHER, s);
+      distill_slots_kernel<<<static_cast<unsigned>(ceil_div(N * q->K, 256)), 256, 0, s>>>(
+          *q, it, N, b0, vb, coef, dp, yk, lse, G, gp);
+      prof_end(K_VOC_TEACHER, s);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    } else if (hipError_t e = launch_vocab_grad_mfma(x, wb, ldw, bc0, b0, n, H, vb, target, lse,
+                                                     dloss, G, gp, s);
+               e != hipSuccess) {
       return e;
+    }
     if (hipError_t e = launch_vocab_dx_mfma(G, gp, wb, ldw, bc0, n, H, vb, kspan, b0 == 0, dxa, s);
         e != hipSuccess)
       return e;
@@ -398,6 +657,30 @@ hipError_t launch_vocab_bwd(const uint16_t* x, const uint16_t* w, const int32_t*
   const int64_t nx = N * H;
   voc_dx_sum_kernel<<<static_cast<unsigned>(ceil_div(nx / 8, 256)), 256, 0, s>>>(dxa, slabs, nx, dx);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_vocab_fwd(const uint16_t* x, const uint16_t* w, const int32_t* target,
+                            int64_t N, int H, int64_t V, int64_t vblock, float* loss, float* lse,
+                            void* ws, size_t ws_bytes, hipStream_t s) {
+  return run_fwd(x, w, target, nullptr, N, H, V, vblock, loss, lse, nullptr, ws, ws_bytes, s);
+}
+hipError_t launch_vocab_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target,
+                            const float* lse, const float* dloss, int64_t N, int H, int64_t V,
+                            int64_t vblock, uint16_t* dx, uint16_t* dw, void* ws, hipStream_t s) {
+  return run_bwd(x, w, target, nullptr, lse, nullptr, dloss, N, H, V, vblock, dx, dw, ws, s);
+}
+hipError_t launch_distill_fwd(const uint16_t* x, const uint16_t* w, const Teacher& q, int64_t N,
+                              int H, int64_t V, int64_t vblock, float* loss, float* lse, float* yk,
+                              void* ws, size_t ws_bytes, hipStream_t s) {
+  return run_fwd(x, w, nullptr, &q, N, H, V, vblock, loss, lse, yk, ws, ws_bytes, s);
+}
+hipError_t launch_distill_bwd(const uint16_t* x, const uint16_t* w, const Teacher& q,
+                              const float* lse, const float* yk, const float* dloss, int64_t N,
+                              int H, int64_t V, int64_t vblock, uint16_t* dx, uint16_t* dw,
+                              void* ws, hipStream_t s) {
+  return run_bwd(x, w, nullptr, &q, lse, yk, dloss, N, H, V, vblock, dx, dw, ws, s);
 }
 
 }  // namespace moe

@@ -481,6 +481,60 @@ def moe_vocab_loss_bwd(x, w_voc, target, lse, dloss, vblock, dx=None, dw_voc=Non
     return dx, dw_voc
 
 
+# ---------------------------------------------------------- distillation
+def _teacher(x, w_voc, topk_idx, topk_logit, vblock, teacher_lse):
+    """(N, H, V, K, workspace) of a distillation call, its arguments checked."""
+    _need(x, torch.bfloat16, "x", 2)
+    _need(topk_idx, torch.int32, "topk_idx", 2)
+    _need(w_voc, torch.bfloat16, "w_voc", 2)
+    N, H = x.shape
+    V = w_voc.shape[1]
+    K = topk_idx.shape[1]
+    _given(x, torch.bfloat16, "x", (N, H))
+    _given(w_voc, torch.bfloat16, "w_voc", (H, V))
+    _given(topk_idx, torch.int32, "topk_idx", (N, K))
+    _given(topk_logit, torch.float32, "topk_logit", (N, K))
+    if teacher_lse is not None:
+        _given(teacher_lse, torch.float32, "teacher_lse", (N,))
+    ws = workspace(_ws_bytes("moe_vocab_distill_workspace_bytes", N, H, V, vblock, K), x.device,
+                   "vocab_distill")
+    return N, H, V, K, ws
+
+
+def moe_vocab_distill_fwd(x, w_voc, topk_idx, topk_logit, vblock, temperature=1.0,
+                          teacher_lse=None, loss=None, lse=None, y_topk=None):
+    """Loss of the vocabulary projection against a teacher's top logits.  x
+    [N,H] bf16, w_voc [H,V] bf16, topk_idx [N,K] int32 (outside [0, V): no
+    slot), topk_logit [N,K] fp32, teacher_lse [N] fp32 (None: the slots'
+    probabilities sum to one).  Returns (loss [N], lse [N], y_topk [N,K]) fp32."""
+    N, H, V, K, ws = _teacher(x, w_voc, topk_idx, topk_logit, vblock, teacher_lse)
+    loss = _out(loss, torch.float32, "loss", (N,), x.device)
+    lse = _out(lse, torch.float32, "lse", (N,), x.device)
+    y_topk = _out(y_topk, torch.float32, "y_topk", (N, K), x.device)
+    _check(lib.moe_vocab_distill_fwd(_ptr(x), _ptr(w_voc), _ptr(topk_idx), _ptr(topk_logit),
+                                     _ptr(teacher_lse), temperature, N, H, V, vblock, K,
+                                     _ptr(loss), _ptr(lse), _ptr(y_topk), _ptr(ws), ws.numel(),
+                                     _stream()), "moe_vocab_distill_fwd")
+    return loss, lse, y_topk
+
+
+def moe_vocab_distill_bwd(x, w_voc, topk_idx, topk_logit, lse, y_topk, dloss, vblock,
+                          temperature=1.0, teacher_lse=None, dx=None, dw_voc=None):
+    """Gradients of the distillation loss given dloss [N] fp32 and the
+    forward's lse and y_topk.  Returns (dx [N,H] bf16, dw_voc [H,V] bf16)."""
+    N, H, V, K, ws = _teacher(x, w_voc, topk_idx, topk_logit, vblock, teacher_lse)
+    _given(lse, torch.float32, "lse", (N,))
+    _given(y_topk, torch.float32, "y_topk", (N, K))
+    _given(dloss, torch.float32, "dloss", (N,))
+    dx = _out(dx, torch.bfloat16, "dx", (N, H), x.device)
+    dw_voc = _out(dw_voc, torch.bfloat16, "dw_voc", (H, V), x.device)
+    _check(lib.moe_vocab_distill_bwd(_ptr(x), _ptr(w_voc), _ptr(topk_idx), _ptr(topk_logit),
+                                     _ptr(teacher_lse), temperature, _ptr(lse), _ptr(y_topk),
+                                     _ptr(dloss), N, H, V, vblock, K, _ptr(dx), _ptr(dw_voc),
+                                     _ptr(ws), ws.numel(), _stream()), "moe_vocab_distill_bwd")
+    return dx, dw_voc
+
+
 # ------------------------------------------ least-loaded expert parallelism
 def moe_llep_plan(counts, E_p, capacity=0, granule=1):
     """Plan of which rank computes which rows of every expert, load counted
