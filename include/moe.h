@@ -361,6 +361,74 @@ int moe_ffn_fwd_row_chunked(const moe_bf16* x, const int32_t* topk_idx, const fl
                             void* workspace, size_t workspace_bytes, void* stream,
                             void* stream2);
 
+/* ------------------------------------------------------------------ MXFP4
+ * The expert layer's forward on 4-bit operands: a frozen layer (a teacher, a
+ * served model) whose expert weights take 17/32 of a byte a value.
+ *
+ * Format (OCP microscaling, MXFP4).  A matrix of `rows` rows along K (a
+ * multiple of 8) is cut into blocks of 32 consecutive k of a row; a block has
+ * one scale byte s, standing for 2^(s - 127) (255: NaN), and 32 codes of four
+ * bits: sign, then 0, 1/2, 1, 3/2, 2, 3, 4, 6 for 0..7.
+ *   q [rows][16 ceil(K / 32)] bytes: two codes a byte, the even k in the low
+ *     half; rows end in zero codes up to a whole block.
+ *   s [ceil(K / 256)][rows][8] bytes: eight blocks' scales of a row together,
+ *     those of blocks 0, 2, 4, 6 first, then 1, 3, 5, 7 (as the matrix
+ *     instruction's lanes take them); 0 for blocks beyond K.
+ * Several matrices (the experts') follow one another in each array.
+ *
+ * moe_mxfp4_bytes: bytes of q and s for B matrices of `rows` rows along K.
+ * moe_mxfp4_quantize: src [B][R][C] bf16 -> B matrices of R rows along C, or,
+ *   with transpose = 1, of C rows along R (expert weights [E][d][f] quantised
+ *   along the contraction d).  A block's scale is 2^(floor(log2 m) - 2), m its
+ *   largest magnitude, clamped to [2^-127, 2^127] (a block of zeros: 2^-127); a
+ *   value is v / scale rounded to the nearest code value, ties to the even
+ *   code, magnitudes above 6 to 6.  A block that holds a NaN or an infinity
+ *   gets scale byte 255 (its codes are then unspecified).  Bit-exact.
+ * moe_mxfp4_dequantize: the values that B matrices stand for, bf16 [B][rows][K]
+ *   (exact: every one is a bf16 value).
+ * Limits: B <= 65535, B * rows < 2^25, K (and with transpose R) as d.
+ */
+int moe_mxfp4_bytes(int64_t B, int64_t rows, int K, size_t* q_bytes, size_t* s_bytes);
+int moe_mxfp4_quantize(const moe_bf16* src, int64_t B, int64_t R, int C, int transpose,
+                       uint8_t* q, uint8_t* s, void* stream);
+int moe_mxfp4_dequantize(const uint8_t* q, const uint8_t* s, int64_t B, int64_t rows, int K,
+                         moe_bf16* dst, void* stream);
+
+/* moe_grouped_swiglu_fwd with MXFP4 operands.  With x^, w^ the values that
+ * the quantised operands stand for, for each row p of expert e's segment:
+ *   h_gate = x^[p] W^_gate[e], h_up = x^[p] W^_up[e]        (fp32 sums)
+ *   a = silu(h_gate) h_up in fp32, quantised to MXFP4 along f (a^)
+ *   y_perm[p] = bf16(a^ W^_down[e])
+ * w_gate, w_up: num_local matrices of f rows along d; w_down: of d rows along
+ * f.  x: one matrix along d of x_rows rows: with row_src (moe_permute's), row p
+ * reads x row row_src[p] / k (x_rows = T: the tokens, quantised once); with
+ * row_src = NULL row p itself (x_rows >= cap).  expert_offsets, cap and y_perm
+ * as for moe_grouped_swiglu_fwd; the rest of its conventions hold.  Limits:
+ * with row_src, x_rows * 16 ceil(d / 32) < 2^31.
+ */
+int moe_grouped_swiglu_mxfp4_workspace_bytes(int64_t cap, int num_local, int d, int f,
+                                             size_t* bytes);
+int moe_grouped_swiglu_fwd_mxfp4(
+    const uint8_t* x_q, const uint8_t* x_s, int64_t x_rows, const int32_t* row_src, int k,
+    const int32_t* expert_offsets, int num_local, int64_t cap, int d, int f,
+    const uint8_t* w_gate_q, const uint8_t* w_gate_s, const uint8_t* w_up_q, const uint8_t* w_up_s,
+    const uint8_t* w_down_q, const uint8_t* w_down_s, moe_bf16* y_perm, void* workspace,
+    size_t workspace_bytes, void* stream);
+
+/* The layer's forward from its routing: the permutation's index (without
+ * gathering rows), x quantised once, moe_grouped_swiglu_fwd_mxfp4 and
+ * moe_combine (weighted by topk_gate) into y [T][d] bf16; tokens with no local
+ * expert get 0.  Arguments otherwise as for moe_ffn_fwd_chunked, one stream;
+ * T < 2^25.
+ */
+int moe_ffn_fwd_mxfp4_workspace_bytes(int64_t T, int E, int k, int num_local, int d, int f,
+                                      size_t* bytes);
+int moe_ffn_fwd_mxfp4(const moe_bf16* x, const int32_t* topk_idx, const float* topk_gate,
+                      int64_t T, int d, int E, int k, int expert_begin, int num_local, int f,
+                      const uint8_t* w_gate_q, const uint8_t* w_gate_s, const uint8_t* w_up_q,
+                      const uint8_t* w_up_s, const uint8_t* w_down_q, const uint8_t* w_down_s,
+                      moe_bf16* y, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------- vocabulary loss
  * Blockwise online loss of the vocabulary projection (Sec. 3.4, eq.
  * (voc-fwd-loss): Y = X W_voc, loss_n = Y[n][t_n] - log sum_v exp Y[n][v]),

@@ -30,6 +30,9 @@ C_SYMBOLS = (
     "moe_combine", "moe_combine_bwd",
     "moe_ffn_fwd_chunked_workspace_bytes", "moe_ffn_fwd_chunked",
     "moe_ffn_fwd_row_chunked_workspace_bytes", "moe_ffn_fwd_row_chunked",
+    "moe_mxfp4_bytes", "moe_mxfp4_quantize", "moe_mxfp4_dequantize",
+    "moe_grouped_swiglu_mxfp4_workspace_bytes", "moe_grouped_swiglu_fwd_mxfp4",
+    "moe_ffn_fwd_mxfp4_workspace_bytes", "moe_ffn_fwd_mxfp4",
     "moe_vocab_loss_workspace_bytes", "moe_vocab_loss_fwd", "moe_vocab_loss_bwd",
     "moe_vocab_distill_workspace_bytes", "moe_vocab_distill_fwd", "moe_vocab_distill_bwd",
     "moe_llep_plan", "moe_llep_dispatch",
@@ -80,6 +83,14 @@ def load(path: str = None):
         "moe_ffn_fwd_row_chunked_workspace_bytes": ([I64, I, I, I, I, I, I64, PSZ], I),
         "moe_ffn_fwd_row_chunked": ([P, P, P, I64, I, I, I, I, I, I, P, P, P, I64, P, P, SZ, P, P],
                                     I),
+        "moe_mxfp4_bytes": ([I64, I64, I, PSZ, PSZ], I),
+        "moe_mxfp4_quantize": ([P, I64, I64, I, I, P, P, P], I),
+        "moe_mxfp4_dequantize": ([P, P, I64, I64, I, P, P], I),
+        "moe_grouped_swiglu_mxfp4_workspace_bytes": ([I64, I, I, I, PSZ], I),
+        "moe_grouped_swiglu_fwd_mxfp4": ([P, P, I64, P, I, P, I, I64, I, I, P, P, P, P, P, P, P, P,
+                                          SZ, P], I),
+        "moe_ffn_fwd_mxfp4_workspace_bytes": ([I64, I, I, I, I, I, PSZ], I),
+        "moe_ffn_fwd_mxfp4": ([P, P, P, I64, I, I, I, I, I, I, P, P, P, P, P, P, P, P, SZ, P], I),
         "moe_vocab_loss_workspace_bytes": ([I64, I, I64, I64, PSZ], I),
         "moe_vocab_loss_fwd": ([P, P, P, I64, I, I64, I64, P, P, P, SZ, P], I),
         "moe_vocab_loss_bwd": ([P, P, P, P, P, I64, I, I64, I64, P, P, P, SZ, P], I),

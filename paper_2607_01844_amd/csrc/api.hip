@@ -90,7 +90,8 @@ const char* const kNames[moe::K_NUM] = {
     "gemm_wgrad_down", "combine",       "combine_bwd",        "route_dlogits",
     "route_dw",     "route_dx",        "vocab_lse",          "vocab_grad",    "llep_plan",     "llep_window",
     "route_split",  "vocab_logits",    "vocab_dx",           "vocab_dw",
-    "balance_part", "balance_sum",     "balance_bwd",        "vocab_teacher"};
+    "balance_part", "balance_sum",     "balance_bwd",        "vocab_teacher",
+    "mx_quantize",  "mx_gate_up",      "mx_down"};
 
 }  // namespace
 
@@ -552,6 +553,138 @@ MOE_API int moe_ffn_fwd_row_chunked(const moe_bf16* x, const int32_t* topk_idx,
                                                     w_down, chunk_rows, y, workspace,
                                                     static_cast<hipStream_t>(stream),
                                                     static_cast<hipStream_t>(stream2)),
+                    fn);
+}
+
+// ---------------------------------------------------------------- MXFP4
+static int check_mx(const char* fn, int64_t B, int64_t R, int C) {
+  CHECK(B >= 0 && B <= 65535, "B out of [0, 65535]");
+  CHECK(R >= 0 && R < (int64_t{1} << 25), "rows out of [0, 2^25)");
+  CHECK(B * R < (int64_t{1} << 25), "B*rows >= 2^25");
+  return check_dim(fn, C, "columns");
+}
+
+MOE_API int moe_mxfp4_bytes(int64_t B, int64_t rows, int K, size_t* q_bytes, size_t* s_bytes) {
+  const char* fn = "moe_mxfp4_bytes";
+  CHECK(q_bytes != nullptr && s_bytes != nullptr, "NULL output");
+  if (int r = check_mx(fn, B, rows, K)) return r;
+  *q_bytes = static_cast<size_t>(B * rows) * (16 * ((K + 31) / 32));
+  *s_bytes = static_cast<size_t>(B * rows) * (8 * ((K + 255) / 256));
+  return MOE_OK;
+}
+
+MOE_API int moe_mxfp4_quantize(const moe_bf16* src, int64_t B, int64_t R, int C, int transpose,
+                               uint8_t* q, uint8_t* s, void* stream) {
+  const char* fn = "moe_mxfp4_quantize";
+  if (int r = check_mx(fn, B, R, C)) return r;
+  CHECK(transpose == 0 || transpose == 1, "transpose must be 0 or 1");
+  if (transpose && B * R > 0) {
+    CHECK(R <= MOE_MAX_DIM, "R > MOE_MAX_DIM with transpose");
+    if (int r = check_dim(fn, static_cast<int>(R), "R")) return r;
+    CHECK(B * C < (int64_t{1} << 25), "B*C >= 2^25 with transpose");
+  }
+  if (B * R > 0) {
+    REQ(src); REQ(q); REQ(s);
+  }
+  return hip_status(moe::launch_mx_quantize(src, B, R, C, transpose, q, s,
+                                            static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+MOE_API int moe_mxfp4_dequantize(const uint8_t* q, const uint8_t* s, int64_t B, int64_t rows, int K,
+                                 moe_bf16* dst, void* stream) {
+  const char* fn = "moe_mxfp4_dequantize";
+  if (int r = check_mx(fn, B, rows, K)) return r;
+  if (B * rows > 0) {
+    REQ(q); REQ(s); REQ(dst);
+  }
+  return hip_status(moe::launch_mx_dequantize(q, s, B, rows, K, dst,
+                                              static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+static int check_mx_ffn(const char* fn, int num_local, int64_t cap, int64_t x_rows, int d, int f) {
+  if (int r = check_ffn(fn, num_local, cap, d, f)) return r;
+  CHECK(x_rows >= 0 && x_rows < (int64_t{1} << 31), "x_rows out of [0, 2^31)");
+  CHECK(x_rows * (16 * ((d + 31) / 32)) <= 0x7ffffff0, "quantised rows of x beyond 2^31 bytes");
+  return MOE_OK;
+}
+
+MOE_API int moe_grouped_swiglu_mxfp4_workspace_bytes(int64_t cap, int num_local, int d, int f,
+                                                     size_t* bytes) {
+  const char* fn = "moe_grouped_swiglu_mxfp4_workspace_bytes";
+  CHECK(bytes != nullptr, "bytes is NULL");
+  if (int r = check_ffn(fn, num_local, cap, d, f)) return r;
+  *bytes = moe::mx_ffn_ws_bytes(cap, num_local, d, f, true);
+  return MOE_OK;
+}
+
+MOE_API int moe_grouped_swiglu_fwd_mxfp4(
+    const uint8_t* x_q, const uint8_t* x_s, int64_t x_rows, const int32_t* row_src, int k,
+    const int32_t* expert_offsets, int num_local, int64_t cap, int d, int f,
+    const uint8_t* w_gate_q, const uint8_t* w_gate_s, const uint8_t* w_up_q, const uint8_t* w_up_s,
+    const uint8_t* w_down_q, const uint8_t* w_down_s, moe_bf16* y_perm, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  const char* fn = "moe_grouped_swiglu_fwd_mxfp4";
+  if (int r = check_mx_ffn(fn, num_local, cap, row_src != nullptr ? x_rows : 0, d, f)) return r;
+  CHECK(k >= 1 && k <= MOE_MAX_K, "k out of [1, MOE_MAX_K]");
+  CHECK(row_src != nullptr || x_rows >= cap, "x_rows < cap without row_src");
+  CHECK(row_src == nullptr || x_rows >= 1 || cap == 0, "x_rows < 1 with row_src");
+  REQ(expert_offsets); REQ(w_gate_q); REQ(w_gate_s); REQ(w_up_q); REQ(w_up_s); REQ(w_down_q);
+  REQ(w_down_s);
+  OPT(row_src);
+  if (cap > 0) {
+    REQ(x_q); REQ(x_s); REQ(y_perm);
+  }
+  if (workspace == nullptr || workspace_bytes < moe::mx_ffn_ws_bytes(cap, num_local, d, f, true))
+    return fail(MOE_ERR_WORKSPACE, fn,
+                "workspace smaller than moe_grouped_swiglu_mxfp4_workspace_bytes()");
+  OPT(workspace);
+  const uint8_t* const wq[3] = {w_gate_q, w_up_q, w_down_q};
+  const uint8_t* const ws[3] = {w_gate_s, w_up_s, w_down_s};
+  return hip_status(moe::launch_mx_ffn(x_q, x_s, x_rows, row_src, k, expert_offsets, num_local, cap,
+                                       d, f, wq, ws, y_perm, workspace,
+                                       static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+MOE_API int moe_ffn_fwd_mxfp4_workspace_bytes(int64_t T, int E, int k, int num_local, int d, int f,
+                                              size_t* bytes) {
+  const char* fn = "moe_ffn_fwd_mxfp4_workspace_bytes";
+  CHECK(bytes != nullptr, "bytes is NULL");
+  if (int r = check_tk(fn, T, E, k)) return r;
+  CHECK(num_local >= 1 && num_local <= E, "num_local out of [1, E]");
+  if (int r = check_mx_ffn(fn, num_local, T * std::min(k, num_local), T, d, f)) return r;
+  *bytes = moe::mx_layer_ws_bytes(T, E, k, num_local, d, f);
+  return MOE_OK;
+}
+
+MOE_API int moe_ffn_fwd_mxfp4(const moe_bf16* x, const int32_t* topk_idx, const float* topk_gate,
+                              int64_t T, int d, int E, int k, int expert_begin, int num_local,
+                              int f, const uint8_t* w_gate_q, const uint8_t* w_gate_s,
+                              const uint8_t* w_up_q, const uint8_t* w_up_s,
+                              const uint8_t* w_down_q, const uint8_t* w_down_s, moe_bf16* y,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "moe_ffn_fwd_mxfp4";
+  if (int r = check_tk(fn, T, E, k)) return r;
+  CHECK(num_local >= 1 && num_local <= E, "num_local out of [1, E]");
+  CHECK(expert_begin >= 0 && expert_begin <= E - num_local, "expert range out of [0, E)");
+  if (int r = check_mx_ffn(fn, num_local, T * std::min(k, num_local), T, d, f)) return r;
+  if (T > 0) {
+    CHECK(T < (int64_t{1} << 25), "T >= 2^25");
+    REQ(x); REQ(topk_idx); REQ(topk_gate); REQ(y);
+    REQ(w_gate_q); REQ(w_gate_s); REQ(w_up_q); REQ(w_up_s); REQ(w_down_q); REQ(w_down_s);
+    if (workspace == nullptr ||
+        workspace_bytes < moe::mx_layer_ws_bytes(T, E, k, num_local, d, f))
+      return fail(MOE_ERR_WORKSPACE, fn,
+                  "workspace smaller than moe_ffn_fwd_mxfp4_workspace_bytes()");
+    OPT(workspace);
+  }
+  const uint8_t* const wq[3] = {w_gate_q, w_up_q, w_down_q};
+  const uint8_t* const ws[3] = {w_gate_s, w_up_s, w_down_s};
+  return hip_status(moe::launch_mx_layer(x, topk_idx, topk_gate, T, d, E, k, expert_begin,
+                                         num_local, f, wq, ws, y, workspace,
+                                         static_cast<hipStream_t>(stream)),
                     fn);
 }
 

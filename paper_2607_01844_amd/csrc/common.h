@@ -95,6 +95,9 @@ enum KernelId {
   K_BALANCE_SUM,
   K_BALANCE_BWD,
   K_VOC_TEACHER,
+  K_MX_QUANT,
+  K_MX_GATE_UP,
+  K_MX_DOWN,
   K_NUM
 };
 
@@ -245,6 +248,26 @@ hipError_t launch_vocab_dx_mfma(const uint16_t* G, int64_t gp, const uint16_t* w
                                 float* dxa, hipStream_t s);
 hipError_t launch_vocab_dw_mfma(const uint16_t* x, const uint16_t* G, int64_t gp, int N, int H,
                                 int vb, uint16_t* dw, int64_t ldd, int64_t cc0, hipStream_t s);
+// Tile tables of the grouped products (see gemm_sched_kernel), [E_loc + 1] each.
+hipError_t launch_gemm_sched(const int32_t* offsets, int E_loc, int rows, int krows,
+                             int32_t* mt_start, int32_t* wk_start, int32_t* nz_start, hipStream_t s);
+// MXFP4: src [B][R][C] bf16 along C (or, transpose, along R) to values q and
+// scales s; back to bf16 [B][rows][K]; the grouped forward on quantised rows
+// (w*[0..2]: gate, up, down); and the layer's from x and its routing.
+hipError_t launch_mx_quantize(const uint16_t* src, int64_t B, int64_t R, int64_t C, int transpose,
+                              uint8_t* q, uint8_t* s, hipStream_t st);
+hipError_t launch_mx_dequantize(const uint8_t* q, const uint8_t* s, int64_t B, int64_t rows,
+                                int64_t K, uint16_t* dst, hipStream_t st);
+size_t mx_ffn_ws_bytes(int64_t cap, int E_loc, int d, int f, bool indirect);
+hipError_t launch_mx_ffn(const uint8_t* xq, const uint8_t* xs, int64_t x_rows,
+                         const int32_t* row_src, int k, const int32_t* offsets, int E_loc,
+                         int64_t cap, int d, int f, const uint8_t* const wq[3],
+                         const uint8_t* const wsc[3], uint16_t* y, void* ws, hipStream_t s);
+size_t mx_layer_ws_bytes(int64_t T, int E, int k, int E_loc, int d, int f);
+hipError_t launch_mx_layer(const uint16_t* x, const int32_t* idx, const float* gate, int64_t T,
+                           int d, int E, int k, int e_begin, int E_loc, int f,
+                           const uint8_t* const wq[3], const uint8_t* const wsc[3], uint16_t* y,
+                           void* ws, hipStream_t s);
 hipError_t launch_ffn_fwd(const uint16_t* x_perm, const int32_t* offsets, int E_loc, int64_t cap,
                           int d, int f, const uint16_t* wg, const uint16_t* wu,
                           const uint16_t* wd, uint16_t* hg, uint16_t* hu, uint16_t* y,

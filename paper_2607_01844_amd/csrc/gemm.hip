@@ -170,14 +170,19 @@ bool keep_large(int64_t cap, int E_loc, int64_t n256, int64_t n128, int64_t K) {
 
 hipError_t sched(const int32_t* offsets, int E_loc, int rows, int krows, const GemmWs& w,
                  hipStream_t s) {
-  prof_begin(K_GEMM_SCHED, s);
-  gemm_sched_kernel<<<1, 1024, 0, s>>>(offsets, E_loc, rows, krows, w.mt_start, w.wk_start,
-                                       w.nz_start);
-  prof_end(K_GEMM_SCHED, s);
-  return hipGetLastError();
+  return launch_gemm_sched(offsets, E_loc, rows, krows, w.mt_start, w.wk_start, w.nz_start, s);
 }
 
 }  // namespace
+
+hipError_t launch_gemm_sched(const int32_t* offsets, int E_loc, int rows, int krows,
+                             int32_t* mt_start, int32_t* wk_start, int32_t* nz_start,
+                             hipStream_t s) {
+  prof_begin(K_GEMM_SCHED, s);
+  gemm_sched_kernel<<<1, 1024, 0, s>>>(offsets, E_loc, rows, krows, mt_start, wk_start, nz_start);
+  prof_end(K_GEMM_SCHED, s);
+  return hipGetLastError();
+}
 
 size_t gemm_ws_bytes(int64_t cap, int E_loc, int d, int f, unsigned flags) {
   (void)d;

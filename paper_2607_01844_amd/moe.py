@@ -435,6 +435,117 @@ def moe_ffn_fwd_row_chunked(x, topk_idx, topk_gate, E, w_gate, w_up, w_down, chu
     return out
 
 
+# ---------------------------------------------------------------- MXFP4
+def _mx_shapes(B, rows, K):
+    """Shapes of the values and scales of B MXFP4 matrices of `rows` rows along K."""
+    return (B, rows, 16 * (-(-K // 32))), (B, -(-K // 256), rows, 8)
+
+
+def moe_mxfp4_quantize(src, transpose=False):
+    """MXFP4 of src [R,C] or [B,R,C] bf16: matrices of R rows along C, or, with
+    transpose, of C rows along R.  Returns (q, s) uint8: q [..., rows,
+    16 ceil(K/32)], s [..., ceil(K/256), rows, 8]."""
+    _need(src, torch.bfloat16, "src")
+    if src.dim() not in (2, 3):
+        raise ValueError(f"src: expected 2 or 3 dims, got {src.dim()}")
+    _given(src, torch.bfloat16, "src", src.shape)
+    B = src.shape[0] if src.dim() == 3 else 1
+    R, C = src.shape[-2:]
+    qs, ss = _mx_shapes(B, *((C, R) if transpose else (R, C)))
+    if src.dim() == 2:
+        qs, ss = qs[1:], ss[1:]
+    q = torch.empty(qs, dtype=torch.uint8, device=src.device)
+    s = torch.empty(ss, dtype=torch.uint8, device=src.device)
+    _check(lib.moe_mxfp4_quantize(_ptr(src), B, R, C, 1 if transpose else 0, _ptr(q), _ptr(s),
+                                  _stream()), "moe_mxfp4_quantize")
+    return q, s
+
+
+def moe_mxfp4_dequantize(q, s, K, out=None):
+    """The values that MXFP4 matrices along K stand for: [..., rows, K] bf16."""
+    _need(q, torch.uint8, "q")
+    if q.dim() not in (2, 3):
+        raise ValueError(f"q: expected 2 or 3 dims, got {q.dim()}")
+    B = q.shape[0] if q.dim() == 3 else 1
+    rows = q.shape[-2]
+    qs, ss = _mx_shapes(B, rows, K)
+    if q.dim() == 2:
+        qs, ss = qs[1:], ss[1:]
+    _given(q, torch.uint8, "q", qs)
+    _given(s, torch.uint8, "s", ss)
+    out = _out(out, torch.bfloat16, "out", (*q.shape[:-1], K), q.device)
+    _check(lib.moe_mxfp4_dequantize(_ptr(q), _ptr(s), B, rows, K, _ptr(out), _stream()),
+           "moe_mxfp4_dequantize")
+    return out
+
+
+def _mx_weights(w_gate, w_up, w_down, d):
+    """(num_local, f, six pointers) of MXFP4 expert weights, each a (q, s) pair."""
+    for name, w in (("w_gate", w_gate), ("w_up", w_up), ("w_down", w_down)):
+        if not isinstance(w, (tuple, list)) or len(w) != 2:
+            raise TypeError(f"{name}: expected the (q, s) pair of moe_mxfp4_quantize")
+    _need(w_gate[0], torch.uint8, "w_gate q", 3)
+    num_local, f = w_gate[0].shape[:2]
+    ptrs = []
+    for name, w, rows, K in (("w_gate", w_gate, f, d), ("w_up", w_up, f, d),
+                             ("w_down", w_down, d, f)):
+        qs, ss = _mx_shapes(num_local, rows, K)
+        ptrs += [_ptr(_given(w[0], torch.uint8, f"{name} q", qs)),
+                 _ptr(_given(w[1], torch.uint8, f"{name} s", ss))]
+    return num_local, f, ptrs
+
+
+def moe_grouped_swiglu_fwd_mxfp4(x, expert_offsets, w_gate, w_up, w_down, d, row_src=None, k=1,
+                                 cap=None, y_perm=None):
+    """Grouped SwiGLU on MXFP4 operands, each a (q, s) pair: x of moe_mxfp4_
+    quantize(x [rows,d]), w_gate and w_up of the transposed [E_loc,d,f], w_down
+    of the transposed [E_loc,f,d].  row_src [cap] int32 (moe_permute's): row p
+    is x row row_src[p] // k; None: row p.  Returns y_perm [cap,d] bf16."""
+    if not isinstance(x, (tuple, list)) or len(x) != 2:
+        raise TypeError("x: expected the (q, s) pair of moe_mxfp4_quantize")
+    _need(x[0], torch.uint8, "x q", 2)
+    x_rows = x[0].shape[0]
+    qs, ss = _mx_shapes(1, x_rows, d)
+    _given(x[0], torch.uint8, "x q", qs[1:])
+    _given(x[1], torch.uint8, "x s", ss[1:])
+    num_local, f, wp = _mx_weights(w_gate, w_up, w_down, d)
+    _given(expert_offsets, torch.int32, "expert_offsets", (num_local + 1,))
+    if row_src is not None:
+        _need(row_src, torch.int32, "row_src", 1)
+        cap = row_src.shape[0] if cap is None else cap
+        _given(row_src, torch.int32, "row_src", (max(cap, 1),))
+    cap = x_rows if cap is None else cap
+    y_perm = _out(y_perm, torch.bfloat16, "y_perm", (max(cap, 1), d), x[0].device)
+    ws = workspace(_ws_bytes("moe_grouped_swiglu_mxfp4_workspace_bytes", cap, num_local, d, f),
+                   x[0].device, "ffn_mxfp4")
+    _check(lib.moe_grouped_swiglu_fwd_mxfp4(_ptr(x[0]), _ptr(x[1]), x_rows, _ptr(row_src), k,
+                                            _ptr(expert_offsets), num_local, cap, d, f, *wp,
+                                            _ptr(y_perm), _ptr(ws), ws.numel(), _stream()),
+           "moe_grouped_swiglu_fwd_mxfp4")
+    return y_perm
+
+
+def moe_ffn_fwd_mxfp4(x, topk_idx, topk_gate, E, w_gate, w_up, w_down, expert_begin=0, out=None):
+    """The expert layer's forward on MXFP4 weights (see moe_grouped_swiglu_fwd_
+    mxfp4) of experts [expert_begin, + num_local).  x [T,d] bf16, topk_idx [T,k]
+    int32, topk_gate [T,k] fp32.  Returns y [T,d] bf16."""
+    _need(x, torch.bfloat16, "x", 2)
+    T, d = x.shape
+    _given(x, torch.bfloat16, "x", (T, d))
+    _need(topk_idx, torch.int32, "topk_idx", 2)
+    k = topk_idx.shape[1]
+    _given(topk_idx, torch.int32, "topk_idx", (T, k))
+    _given(topk_gate, torch.float32, "topk_gate", (T, k))
+    num_local, f, wp = _mx_weights(w_gate, w_up, w_down, d)
+    out = _out(out, torch.bfloat16, "out", (T, d), x.device)
+    ws = workspace(_ws_bytes("moe_ffn_fwd_mxfp4_workspace_bytes", T, E, k, num_local, d, f),
+                   x.device, "ffn_fwd_mxfp4")
+    _check(lib.moe_ffn_fwd_mxfp4(_ptr(x), _ptr(topk_idx), _ptr(topk_gate), T, d, E, k,
+                                 expert_begin, num_local, f, *wp, _ptr(out), _ptr(ws), ws.numel(),
+                                 _stream()), "moe_ffn_fwd_mxfp4")
+    return out
+
+
 # ------------------------------------------------------- vocabulary loss
 def _vocab_ws(N, H, V, vblock, device):
     return workspace(_ws_bytes("moe_vocab_loss_workspace_bytes", N, H, V, vblock), device,
