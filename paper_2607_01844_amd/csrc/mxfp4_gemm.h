@@ -58,7 +58,8 @@ struct MxGeom {
   static constexpr int NWAVE = S / 32, NTHR = 64 * NWAVE, AIM = S / 64;
   static constexpr int PATCH = 2048;    // per wave, of the bf16 output
   static constexpr int SCALES = 4 * UNIT, PATCHES = SCALES + 4 * SUNIT;
-  static constexpr int LDS = PATCHES + NWAVE * PATCH;  // 152 KiB, or 76 KiB
+  static constexpr int TOKENS = PATCHES + NWAVE * PATCH;  // tokens of each wave's rows
+  static constexpr int LDS = TOKENS + NWAVE * 256;        // 154 KiB, or 77 KiB
 };
 
 // 4 bytes per lane, global -> LDS (see load_lds16)
@@ -112,15 +113,26 @@ struct MxStream {
   __device__ __forceinline__ void none() {
     chunks = 0;
     srange = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) voff[q] = OOB;
   }
-  // no branches: one in the middle of a step would let the compiler gather the
-  // step's matrix instructions behind it
+  // Step j's values into the LDS unit at `u`.  TAIL: chunks past the row's end
+  // read as zeros; of two operands one that does is enough, since the other's
+  // then meet zeros (codes are finite whatever the bytes).  No branches: one in
+  // the middle of a step would let the compiler gather the step's matrix
+  // instructions behind it.
+  template <bool TAIL>
   __device__ __forceinline__ void values(int j, uint32_t u, int w, int lane) const {
     const uint32_t kb = static_cast<uint32_t>(j) * 128u;
-    const int lc0 = (lane & 7) ^ (lane >> 4);  // chunk of loads 0 and 2; of 1 and 3 lc0 ^ 4
-    const bool in[2] = {lc0 < chunks - 8 * j, (lc0 ^ 4) < chunks - 8 * j};
+    if constexpr (TAIL) {
+      const int lc0 = (lane & 7) ^ (lane >> 4);  // chunk of loads 0 and 2; of 1 and 3 lc0 ^ 4
+      const bool in[2] = {lc0 < chunks - 8 * j, (lc0 ^ 4) < chunks - 8 * j};
 #pragma unroll
-    for (int q = 0; q < 4; ++q) load_lds16(rs, in[q & 1] ? voff[q] + kb : OOB, u + (4 * w + q) * 1024);
+      for (int q = 0; q < 4; ++q) load_lds16(rs, in[q & 1] ? voff[q] + kb : OOB, u + (4 * w + q) * 1024);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) load_lds16(rs, voff[q] + kb, u + (4 * w + q) * 1024);
+    }
   }
   __device__ __forceinline__ void scales(int j, uint32_t u, int w, int lane) const {
     const uint64_t a = sbase + static_cast<uint64_t>(j) * sstep;
@@ -130,6 +142,59 @@ struct MxStream {
     r[2] = static_cast<int>(srange);
     r[3] = 0x00020000;
     load_lds4(r, static_cast<uint32_t>(4 * lane), u + w * 256);
+  }
+};
+
+// Accumulators that have to be there at this point: keeps the matrix
+// instructions before it from being moved behind the branches that follow.
+__device__ __forceinline__ void pin(f32x16& v) { asm volatile("" : "+v"(v)); }
+
+// One tile: rows [row0, row0 + rows) (permuted rows, at most 32 h) of expert e,
+// output columns from n0.
+struct MxTile {
+  int valid, e, row0, rows, h, n0;
+};
+
+// The tiles of one workgroup, in the order of the bf16 row-grouped products'
+// (TileIter), 64 at a time: lane i finds tile 64 b + i once, and a tile is read
+// from the lanes when its turn comes.  (Found one by one, with a chain of
+// scalar loads each, a tile took 4000 cycles of a gate/up product's 60,000.)
+template <int S, bool DUAL>
+struct MxList {
+  int L0, stride, count;  // first tile, step, number of this workgroup's tiles
+  int e, row0, rows, h, n0;  // of lane's tile
+  __device__ __forceinline__ void init(int total) {
+    const int xcd = blockIdx.x % NXCD;
+    stride = gridDim.x / NXCD;
+    const int per = (total + NXCD - 1) / NXCD;
+    L0 = xcd * per + blockIdx.x / NXCD;
+    const int end = min((xcd + 1) * per, total);
+    count = L0 < end ? (end - 1 - L0) / stride + 1 : 0;
+  }
+  // tiles from, from + 1, ...; mt(i), off(i): entries of the tables
+  template <typename MT, typename OFF>
+  __device__ __forceinline__ void fill(int from, int E_loc, int NT, int lane, MT&& mt, OFF&& off) {
+    const int i = min(from + lane, count - 1);
+    const int L = L0 + i * stride;
+    int lo = 0, hi = E_loc;
+    while (hi - lo > 1) {  // the same number of turns in every lane, up to one
+      const int mid = (lo + hi) >> 1;
+      if (mt(mid) * NT <= L) lo = mid; else hi = mid;
+    }
+    const int m = mt(lo), mts = mt(lo + 1) - m;
+    const int seg = off(lo), ne = off(lo + 1) - seg;
+    int tm, tn;
+    tile_pos<4>(L - m * NT, mts, NT, tm, tn);
+    e = lo;
+    h = tile_blocks(ne, mts);
+    const int m0 = tm * 32 * h;
+    row0 = seg + m0;
+    rows = min(ne - m0, 32 * h);
+    n0 = tn * (DUAL ? S / 2 : S);
+  }
+  __device__ __forceinline__ MxTile get(int i) const {
+    auto at = [i](int v) { return __builtin_amdgcn_readlane(v, i & 63); };
+    return MxTile{i < count, at(e), at(row0), at(rows), at(h), at(n0)};
   }
 };
 
@@ -153,7 +218,6 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
   using G = MxGeom<S>;
   constexpr bool DUAL = MODE == MX_GATE_UP;
   constexpr int UNIT = G::UNIT, SUNIT = G::SUNIT, NWAVE = G::NWAVE, AIM = G::AIM;
-  constexpr int WALK = DUAL ? FWD_GATE_UP : FWD_DOWN;  // the bf16 products' tiles
   __shared__ __align__(1024) char lds[G::LDS];
   lds_char* const ring = (lds_char*)(lds);
   const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring));
@@ -165,32 +229,91 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
   const int kq = (K + 31) / 32 * 16, nk = (K + 255) / 256;
   const int64_t wbytes = static_cast<int64_t>(N) * kq, sbytes = static_cast<int64_t>(nk) * N * 8;
 
-  Tables<S> tb{g.t.mt_start, g.t.offsets, g.t.wk_start, g.t.nz_start};
-  tb.init(g.t.E_loc, lane);
-
   // ------------------------------------------------------------ loads
-  TileIter<WALK, S> lit;  // the loads' walk over the tiles, ahead of the products'
-  lit.init(g.t, tb);
+  // They run ahead of the products, two steps of K: at most two tiles (of one
+  // step), which wait here for their turn.
+  MxList<S, DUAL> list;
+  {
+    // the tables pass through the ring, which is not in use yet
+    int* const mt = reinterpret_cast<int*>(lds);
+    int* const off = mt + g.t.E_loc + 1;
+    for (int i = threadIdx.x; i <= g.t.E_loc; i += G::NTHR) {
+      mt[i] = g.t.mt_start[i];
+      off[i] = g.t.offsets[i];
+    }
+    __syncthreads();
+    list.init(__builtin_amdgcn_readfirstlane(mt[g.t.E_loc] * g.t.NT));
+    if (list.count > 0)
+      list.fill(0, g.t.E_loc, g.t.NT, lane, [&](int i) { return mt[i]; }, [&](int i) { return off[i]; });
+    __syncthreads();
+  }
+  if (list.count == 0) return;
+  MxTile q1{}, q2{};
+  int queued = 0, li = 0;  // tiles waiting; the next one to load
+  auto push = [&](const MxTile& t) __attribute__((always_inline)) {
+    const bool one = queued == 0;
+    auto pick = [one](int& a, int& b, int v) __attribute__((always_inline)) {
+      a = one ? v : a;
+      b = one ? b : v;
+    };
+    pick(q1.valid, q2.valid, t.valid);
+    pick(q1.e, q2.e, t.e);
+    pick(q1.row0, q2.row0, t.row0);
+    pick(q1.rows, q2.rows, t.rows);
+    pick(q1.h, q2.h, t.h);
+    pick(q1.n0, q2.n0, t.n0);
+    ++queued;
+  };
+  auto pop = [&]() __attribute__((always_inline)) {
+    const MxTile t = q1;
+    q1 = q2;
+    --queued;
+    return t;
+  };
+  // the tokens of this wave's rows of a tile, on their way to LDS
+  auto load_tokens = [&](const MxTile& t, int lane) __attribute__((always_inline)) {
+    const int rows = t.rows - 32 * w;
+    load_lds4(make_rsrc(g.a_tok + t.row0 + 32 * w, 4 * min(rows, 32)), 4 * lane, lds0 + G::TOKENS + w * 256);
+  };
   MxStream sa, sb;
-  int lstep = nk;     // the next step to load of the loads' tile (nk: take the next tile)
+  int lstep = 0;  // the next step to load of the loads' tile
   auto load_tile = [&]() __attribute__((always_inline)) {
-    const Tile t = lit.next(g.t, tb);
     lstep = 0;
-    if (!t.valid) {
+    if (li >= list.count) {
       sa.none();
       sb.none();
+      if (queued < 2) push(MxTile{0, 0, 0, 0, 0, 0});  // the end (never more than one is read)
       return;
     }
+    const int lane = opaque(threadIdx.x & 63);
+    const bool fresh = (li & 63) == 0;
+    if (fresh && li > 0)
+      list.fill(li, g.t.E_loc, g.t.NT, lane, [&](int i) { return g.t.mt_start[i]; },
+                [&](int i) { return g.t.offsets[i]; });
+    const MxTile t = list.get(li);
+    push(t);
     {
-      const int64_t r0 = static_cast<int64_t>(t.seg) + t.m0 + 32 * w;
-      const int rows = min(t.ne - t.m0, 32 * t.h) - 32 * w;
+      const int rows = t.rows - 32 * w;
+      const int64_t r0 = static_cast<int64_t>(t.row0) + 32 * w;
       if (g.a_tok != nullptr) {
-        const int32_t* tok = g.a_tok + r0;
-        sa.setup(g.a.q, g.a_bytes, kq, rows, [&](int r) { return r < rows ? tok[r] : 0; }, g.a.s, g.a_rows,
-                 r0, lane);
+        if (fresh) {
+          load_tokens(t, lane);
+          wait_vmcnt<0>();
+        }
+        const lds_char* tok = ring + G::TOKENS + w * 256;
+        sa.setup(g.a.q, g.a_bytes, kq, rows,
+                 [&](int r) { return *reinterpret_cast<const __attribute__((address_space(3))) int*>(tok + 4 * r); },
+                 g.a.s, g.a_rows, r0, lane);
+        ++li;
+        // the next tile's, which the waits between land before its turn
+        if (li < list.count && (li & 63) != 0) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          load_tokens(list.get(li), lane);
+        }
       } else {
         sa.setup(g.a.q + r0 * kq, static_cast<int64_t>(rows) * kq, kq, rows, [](int r) { return r; }, g.a.s,
                  g.a_rows, r0, lane);
+        ++li;
       }
     }
     {
@@ -201,15 +324,17 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
                [](int r) { return r; }, b.s + t.e * sbytes, N, n0, lane);
     }
   };
-  // part p (0: A's values, 1: B's, 2: scales) of the step `lstep` into slot `slot`
-  auto load_part = [&](int slot, int p) __attribute__((always_inline)) {
+  // parts of the step `lstep` into slot `slot`
+  auto load_a = [&](int slot) __attribute__((always_inline)) {
+    sa.template values<false>(lstep, lds0 + slot * UNIT, w, 0);
+  };
+  auto load_b = [&](int slot) __attribute__((always_inline)) {
+    sb.template values<true>(lstep, lds0 + (2 + slot) * UNIT, w, opaque(threadIdx.x & 63));
+  };
+  auto load_s = [&](int slot) __attribute__((always_inline)) {
     const int ln = opaque(threadIdx.x & 63);
-    if (p == 0) sa.values(lstep, lds0 + slot * UNIT, w, ln);
-    else if (p == 1) sb.values(lstep, lds0 + (2 + slot) * UNIT, w, ln);
-    else {
-      sa.scales(lstep, lds0 + G::SCALES + slot * SUNIT, w, ln);
-      sb.scales(lstep, lds0 + G::SCALES + (2 + slot) * SUNIT, w, ln);
-    }
+    sa.scales(lstep, lds0 + G::SCALES + slot * SUNIT, w, ln);
+    sb.scales(lstep, lds0 + G::SCALES + (2 + slot) * SUNIT, w, ln);
   };
 
   // --------------------------------------------------------- products
@@ -225,28 +350,29 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
 #pragma unroll
         for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
   };
-  struct Frags {
-    i32x4v a[AIM], b[2];
-  };
   struct Scales {
     int a[AIM], b[2];
   };
+  typedef const __attribute__((address_space(3))) i32x4v* lds_frag;
+  i32x4v fa[2][AIM], fb[4][2];  // fragments: A's of a sub-step and the next, B's of a whole step
   int fl = lane;  // the lane, made opaque tile by tile: addresses of one row-block
                   // count are not kept live through another's loop
-  // fragment f (0 .. AIM - 1: A's row blocks, then B's two) of sub-step `sub`
-  auto load_frag1 = [&](Frags& F, int slot, int sub, auto FI) __attribute__((always_inline)) {
-    constexpr int fi = FI;
-    if constexpr (fi < AIM) {
-      const lds_char* t = ring + slot * UNIT + (arow0 + 32 * fi) * 128;
-      F.a[fi] = *reinterpret_cast<const __attribute__((address_space(3))) i32x4v*>(t + koff(fl & 31, 2 * sub + (fl >> 5)));
-    } else {
-      const lds_char* t = ring + (2 + slot) * UNIT + brow[fi - AIM] * 128;
-      F.b[fi - AIM] = *reinterpret_cast<const __attribute__((address_space(3))) i32x4v*>(t + koff(fl & 31, 2 * sub + (fl >> 5)));
-    }
+  auto load_fa = [&](int slot, auto SUB, auto I) __attribute__((always_inline)) {
+    const lds_char* t = ring + slot * UNIT + (arow0 + 32 * I) * 128;
+    fa[SUB & 1][I] = *reinterpret_cast<lds_frag>(t + koff(fl & 31, 2 * SUB + (fl >> 5)));
   };
-  auto load_frags = [&](Frags& F, int slot, int sub, auto AIC) __attribute__((always_inline)) {
-    static_for<AIM + 2>([&](auto FI) {
-      if constexpr (FI >= AIM || FI < AIC) load_frag1(F, slot, sub, FI);
+  auto load_fb = [&](int slot, auto SUB, auto J) __attribute__((always_inline)) {
+    const lds_char* t = ring + (2 + slot) * UNIT + brow[J] * 128;
+    fb[SUB][J] = *reinterpret_cast<lds_frag>(t + koff(fl & 31, 2 * SUB + (fl >> 5)));
+  };
+  // the first sub-step's fragments of a step
+  auto load_first = [&](int slot, auto AIC) __attribute__((always_inline)) {
+    constexpr std::integral_constant<int, 0> Z{};
+    load_fa(slot, Z, Z);
+    load_fb(slot, Z, Z);
+    load_fb(slot, Z, std::integral_constant<int, 1>{});
+    static_for<AIM>([&](auto I) {
+      if constexpr (I > 0 && I < AIC) load_fa(slot, Z, I);
     });
   };
   auto load_scales = [&](Scales& c, int slot, auto AIC) __attribute__((always_inline)) {
@@ -259,25 +385,35 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
     for (int j = 0; j < 2; ++j)
       c.b[j] = *reinterpret_cast<const __attribute__((address_space(3))) int*>(s + 2 * SUNIT + brow[j] * 8);
   };
-  auto mma1 = [&](const Frags& F, const Scales& c, auto SUB, auto T) __attribute__((always_inline)) {
-    constexpr int i = T / 2, j = T % 2;
-    const i32x8 bv = __builtin_shufflevector(F.b[j], F.b[j], 0, 1, 2, 3, -1, -1, -1, -1);
-    const i32x8 av = __builtin_shufflevector(F.a[i], F.a[i], 0, 1, 2, 3, -1, -1, -1, -1);
+  auto mma1 = [&](const Scales& c, auto SUB, auto T) __attribute__((always_inline)) {
+    constexpr int i = T / 2, j = T % 2, p = SUB & 1;
+    const i32x8 bv = __builtin_shufflevector(fb[SUB][j], fb[SUB][j], 0, 1, 2, 3, -1, -1, -1, -1);
+    const i32x8 av = __builtin_shufflevector(fa[p][i], fa[p][i], 0, 1, 2, 3, -1, -1, -1, -1);
     acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bv, av, acc[i][j], 4, 4, SUB, c.b[j], SUB, c.a[i]);
+    __builtin_amdgcn_sched_barrier(0);
   };
-  // the 2 AI products of sub-step SUB, with the next sub-step's fragment reads
-  // between them in the order that its products need them
-  auto mma_read = [&](const Frags& F, Frags& Gn, const Scales& c, int slot, auto SUB, auto AIC)
-      __attribute__((always_inline)) {
-    constexpr int AI = AIC, per = AI == 1 ? 2 : 1;
+  // The 2 AI products of sub-step SUB.  Between them go the fragment reads of
+  // A's next sub-step (and in sub-step 0 all the rest of B's), spread evenly,
+  // and extra() halfway.
+  auto mma_read = [&](const Scales& c, int slot, auto SUB, auto AIC, auto&& extra) __attribute__((always_inline)) {
+    constexpr int AI = AIC, n = AI + (SUB == 0 ? 6 : 0);  // reads
     static_for<2 * AI>([&](auto T) {
-      mma1(F, c, SUB, T);
-      __builtin_amdgcn_sched_barrier(0);
-      static_for<per>([&](auto P) {
-        constexpr int r = per * T + P;
-        if constexpr (r < AI + 2) {
-          constexpr int f0 = r == 0 ? 0 : r == 1 ? AIM : r == 2 ? AIM + 1 : r - 2;
-          load_frag1(Gn, slot, SUB + 1, std::integral_constant<int, f0>{});
+      mma1(c, SUB, T);
+      if constexpr (T == AI) {
+        extra();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      static_for<n>([&](auto R) {
+        constexpr int r = R;
+        if constexpr (r * 2 * AI / n == T) {
+          // A's first fragment, B's (the next sub-step's first), then A's others
+          if constexpr (SUB == 0) {
+            if constexpr (r >= 1 && r < 7)
+              load_fb(slot, std::integral_constant<int, 1 + (r - 1) / 2>{}, std::integral_constant<int, (r - 1) % 2>{});
+            else load_fa(slot, std::integral_constant<int, 1>{}, std::integral_constant<int, r == 0 ? 0 : r - 6>{});
+          } else {
+            load_fa(slot, std::integral_constant<int, SUB + 1>{}, R);
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
       });
@@ -286,27 +422,26 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
 
   // --------------------------------------------------------- epilogue
   // acc[i][j][4 q + u]: output row arow0 + 32 i + l32, column brow[j] + 8 q + 4 lh + u
-  auto epilogue = [&](const Tile& tl, int ai) __attribute__((always_inline)) {
-    const int mvalid = min(tl.ne - tl.m0, 32 * tl.h);
-    const int64_t row0 = static_cast<int64_t>(tl.seg) + tl.m0;
+  auto epilogue = [&](const MxTile& tl, int ai) __attribute__((always_inline)) {
+    const int mvalid = tl.rows;
+    const int64_t row0 = tl.row0;
     // lane-derived indices formed here, not kept live across the K loop
     const int lane = opaque(threadIdx.x & 63), l32 = lane & 31, lh = lane >> 5;
     static_for<AIM>([&](auto I) {
       constexpr int i = I;
       if (i >= ai) return;
       const int rb = arow0 + 32 * i;
-      if (rb >= mvalid) return;
       if constexpr (DUAL) {
         // The wave's 32 columns of a row are one block of the down product's
         // contraction: lanes l and l + 32 hold 16 each.
         const int col = tl.n0 + wn * 32;
-        if (col >= f) return;
         float a[16];
         uint32_t top = 0;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
+          // silu by the hardware's exponential and reciprocal (each within 2^-22)
           const float z = acc[i][0][r];
-          a[r] = z * sigmoidf_fast(z) * acc[i][1][r];
+          a[r] = z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)) * acc[i][1][r];
           top = max(top, __float_as_uint(a[r]) & 0x7fffffffu);
         }
         top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32, 64)));
@@ -324,8 +459,9 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
         }
         const uint32_t o0 = static_cast<uint32_t>(__shfl_xor(static_cast<int>(p[0]), 32, 64));
         const uint32_t o1 = static_cast<uint32_t>(__shfl_xor(static_cast<int>(p[1]), 32, 64));
+        if constexpr (i == 0) wait_vmcnt<0>();  // see front(): loads that the next step reads
         const int rt = rb + l32;
-        if (lh == 0 && rt < mvalid) {
+        if (lh == 0 && rt < mvalid && col < f) {
           const int64_t row = row0 + rt;
           const int fq = (f + 31) / 32 * 16, b = col / 32, nb = (f + 31) / 32;
           *reinterpret_cast<uint4*>(g.act_q + row * fq + col / 2) =
@@ -359,74 +495,92 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
             });
           }
           asm volatile("" ::: "memory");
+          u32x4v v[2];
           static_for<2>([&](auto Tt) {
             constexpr int t = Tt;
             const int r = 8 * t + (lane >> 3), c = lane & 7;
-            const u32x4v v = *(__attribute__((address_space(3))) u32x4v*)(patch + r * 128 +
-                                                                          ((c ^ ((r >> 1) & 7)) << 4));
+            v[t] = *(__attribute__((address_space(3))) u32x4v*)(patch + r * 128 + ((c ^ ((r >> 1) & 7)) << 4));
+          });
+          asm volatile("" ::: "memory");
+          if constexpr (i == 0 && h == 0) wait_vmcnt<0>();  // see front()
+          static_for<2>([&](auto Tt) {
+            constexpr int t = Tt;
+            const int r = 8 * t + (lane >> 3), c = lane & 7;
             const int rt = rb + 16 * h + r, col = tl.n0 + wn * 64 + 8 * c;
             if (rt < mvalid && col < d) {
               uint16_t* const to = g.y + (row0 + rt) * d + col;
-              if ((d & 63) == 0) store_perm<true>(to, make_uint4(v[0], v[1], v[2], v[3]));
-              else store_perm<false>(to, make_uint4(v[0], v[1], v[2], v[3]));
+              const uint4 o = make_uint4(v[t][0], v[t][1], v[t][2], v[t][3]);
+              if ((d & 63) == 0) store_perm<true>(to, o);
+              else store_perm<false>(to, o);
             }
           });
-          asm volatile("" ::: "memory");
         });
       }
     });
   };
 
   // -------------------------------------------------------- tile stream
-  TileIter<WALK, S> it;
-  it.init(g.t, tb);
-  Tile tc = it.next(g.t, tb);
-  if (!tc.valid) return;
-  // step 0 into slot 0, step 1 into slot 1
-  auto load_step = [&](int slot) __attribute__((always_inline)) {
-    if (lstep == nk) load_tile();
-    load_part(slot, 0);
-    load_part(slot, 1);
-    load_part(slot, 2);
-    ++lstep;
-  };
-  load_step(0);
+  load_tile();  // step 0 into slot 0, step 1 into slot 1
+  MxTile tc = pop();
+  load_a(0);
+  load_b(0);
+  load_s(0);
+  ++lstep;
   wait_vmcnt<0>();
-  load_step(1);
+  if (nk == 1) load_tile();
+  load_a(1);
+  load_b(1);
+  load_s(1);
+  ++lstep;
+  wait_vmcnt<0>();  // (step 1 too: a tile's first step waits for no loads)
   lgkm_drained();
   __builtin_amdgcn_s_barrier();
   __builtin_amdgcn_sched_barrier(0);
 
-  Frags cur, nxt;
   Scales sc, sn;
   int slot = 0;
+  auto nothing = []() {};
   zero_acc();
   while (true) {
-    auto step = [&](auto AIC) __attribute__((always_inline)) {
-      constexpr int AI = AIC;
-      if (lstep == nk) load_tile();
-      mma_read(cur, nxt, sc, slot, std::integral_constant<int, 0>{}, AIC);
-      mma_read(nxt, cur, sc, slot, std::integral_constant<int, 1>{}, AIC);
-      mma_read(cur, nxt, sc, slot, std::integral_constant<int, 2>{}, AIC);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's reads of the slot are done
-      wait_vmcnt<0>();                                    // and the next step has landed
+    // Sub-steps 0 to 2 of the step in `slot`.  B's fragments of all four are read
+    // in sub-step 0 and a barrier then frees B's slot, so that B (the weights,
+    // which come from further away) is loaded one step and a half ahead of its
+    // use where A is one; A's and B's loads thus go out half a step apart.  At the
+    // end every wave has read A's slot, and the next step's values have landed:
+    // all loads but the six of B and the scales that this step issued.  FIRST:
+    // the tile's first step, whose next step was loaded before the epilogue's
+    // stores and waited for there, so that its end does not wait for the stores.
+    auto front = [&](auto AIC, auto FIRST) __attribute__((always_inline)) {
+      mma_read(sc, slot, std::integral_constant<int, 0>{}, AIC, nothing);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
+      mma_read(sc, slot, std::integral_constant<int, 1>{}, AIC, [&]() __attribute__((always_inline)) {
+        load_b(slot);
+        load_s(slot);
+      });
+      mma_read(sc, slot, std::integral_constant<int, 2>{}, AIC, nothing);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's reads of the slot are done
+      if constexpr (!FIRST) wait_vmcnt<6>();              // and the next step has landed
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // Sub-step 3, from registers, with the next step's first fragments and A's
+    // loads into the slot just read.  LAST: before the epilogue.
+    auto back = [&](auto AIC, auto LAST) __attribute__((always_inline)) {
+      constexpr int AI = AIC;
       lgkm_drained();
-      load_scales(sn, slot ^ 1, AIC);
-      load_frags(cur, slot ^ 1, 0, AIC);
+      if constexpr (!LAST) {
+        load_scales(sn, slot ^ 1, AIC);
+        load_first(slot ^ 1, AIC);
+      }
       __builtin_amdgcn_sched_barrier(0);
       static_for<2 * AI>([&](auto T) {
-        constexpr int t = T;
-        mma1(nxt, sc, std::integral_constant<int, 3>{}, T);
-        __builtin_amdgcn_sched_barrier(0);
-        static_for<3>([&](auto P) {
-          constexpr int p = P;
-          if constexpr (p * 2 * AI / 3 == t) {
-            load_part(slot, p);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        });
+        mma1(sc, std::integral_constant<int, 3>{}, T);
+        if constexpr (T == 0) {
+          load_a(slot);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       });
       ++lstep;
       lgkm_drained();
@@ -434,12 +588,35 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
       sc = sn;
       slot ^= 1;
     };
+    using T_ = std::true_type;
+    using F_ = std::false_type;
     auto k_loop = [&](auto AIC) __attribute__((always_inline)) {
       fl = opaque(threadIdx.x & 63);
       lgkm_drained();
       load_scales(sc, slot, AIC);
-      load_frags(cur, slot, 0, AIC);
-      for (int ks = 0; ks < nk; ++ks) step(AIC);
+      load_first(slot, AIC);
+      // the loads are two steps ahead: from step nk - 2 on they are the next
+      // tile's (or, of tiles of one step, always another's)
+      if (nk <= 2) load_tile();
+      front(AIC, T_{});
+      if (nk > 1) {
+        back(AIC, F_{});
+        if (nk > 2) {
+          for (int ks = 1; ks + 2 < nk; ++ks) {
+            front(AIC, F_{});
+            back(AIC, F_{});
+          }
+          static_for<AIC>([&](auto I) {
+            pin(acc[I][0]);
+            pin(acc[I][1]);
+          });
+          load_tile();
+          front(AIC, F_{});
+          back(AIC, F_{});
+        }
+        front(AIC, F_{});
+      }
+      back(AIC, T_{});
     };
     const int ai = wm == 0 ? (tc.h + 1) >> 1 : tc.h >> 1;
     arow0 = wm == 0 ? 0 : 32 * ((tc.h + 1) >> 1);
@@ -447,7 +624,7 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
       if (ai == I + 1) k_loop(std::integral_constant<int, I + 1>{});
     });
     epilogue(tc, ai);
-    tc = it.next(g.t, tb);
+    tc = pop();
     if (!tc.valid) break;
     zero_acc();
   }
