@@ -30,35 +30,97 @@ __device__ __forceinline__ uint32_t pair_top(uint32_t v) {
   return max((v << 16) & 0x7fffffffu, v & 0x7fff0000u);
 }
 
+// Quantised rows on their way into a layer: each token's scales go to its
+// permuted rows, whose token is noted (dst: see moe_permute), and the last
+// workgroup forms the table of row tiles of the products that follow.
+struct Scatter {
+  const int32_t* dst;      // [T][k]; null: scales stay in row order
+  const int32_t* offsets;  // [E_loc + 1]
+  int32_t *tok, *mt;       // [cap], [E_loc + 1]
+  int64_t cap;
+  int k, E_loc, tile;      // tile: rows of a row tile
+};
+
+// mt[e] = row tiles of the experts before e (256 threads, up to 1024 experts).
+__device__ __forceinline__ void tile_table(const Scatter& c) {
+  __shared__ int wsum[4];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int v[4], sum = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = 4 * threadIdx.x + i;
+    v[i] = e < c.E_loc ? (c.offsets[e + 1] - c.offsets[e] + c.tile - 1) / c.tile : 0;
+    sum += v[i];
+  }
+  int incl = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int u = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 63) wsum[w] = incl;
+  __syncthreads();
+  int at = incl - sum;
+  for (int q = 0; q < w; ++q) at += wsum[q];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int e = 4 * threadIdx.x + i;
+    if (e < c.E_loc) c.mt[e] = at;
+    at += v[i];
+    if (e == c.E_loc - 1) c.mt[c.E_loc] = at;
+  }
+}
+
 // Along rows: q [rows][kq], s [ceil(K / 256)][rows][8] of src [rows][K] (batches
-// of `rows` rows follow one another).  Four lanes a block, 8 values each; W
-// lanes along K, the rest of the workgroup along rows.
-template <int W>
+// of `rows` rows follow one another).  Four lanes a block, 8 values each, 32 the
+// eight blocks whose scales lie together; W lanes along K, the rest of the
+// workgroup along rows.  SCATTER: the scales go to s [ceil(K / 256)][cap][8].
+template <int W, bool SCATTER>
 __global__ __launch_bounds__(256) void mx_quant_kernel(const uint16_t* __restrict__ src, int64_t total,
                                                        int64_t rows, int K, uint8_t* __restrict__ q,
-                                                       uint8_t* __restrict__ s) {
+                                                       uint8_t* __restrict__ s, Scatter sc) {
   constexpr int RPB = 256 / W;
+  if constexpr (SCATTER) {
+    if (blockIdx.x == gridDim.x - 1) {
+      if (blockIdx.y == 0) tile_table(sc);
+      return;
+    }
+  }
   const int nb = (K + 31) / 32, nkg = (nb + 7) / 8;
   const int u = blockIdx.y * W + threadIdx.x % W;  // 8 values of the row
   const int b = u >> 2, part = u & 3;
   const int64_t r = static_cast<int64_t>(blockIdx.x) * RPB + threadIdx.x / W;
-  if (r >= total || b >= 8 * nkg) return;  // whole groups of four lanes
+  if (r >= total || b >= 8 * nkg) return;  // whole groups of 32 lanes
   uint4 v = make_uint4(0u, 0u, 0u, 0u);
   if (8 * u < K) v = *reinterpret_cast<const uint4*>(src + r * K + 8 * u);
   uint32_t top = max(max(pair_top(v.x), pair_top(v.y)), max(pair_top(v.z), pair_top(v.w)));
   top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 1, 64)));
   top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 2, 64)));
   const uint32_t e8 = mx_scale(top);
-  const float sc = __uint_as_float(e8 << 23);
+  const float scale = __uint_as_float(e8 << 23);
   uint32_t o = 0;
-  o = fp4_pair_bf16<0>(o, v.x, sc);
-  o = fp4_pair_bf16<1>(o, v.y, sc);
-  o = fp4_pair_bf16<2>(o, v.z, sc);
-  o = fp4_pair_bf16<3>(o, v.w, sc);
+  o = fp4_pair_bf16<0>(o, v.x, scale);
+  o = fp4_pair_bf16<1>(o, v.y, scale);
+  o = fp4_pair_bf16<2>(o, v.z, scale);
+  o = fp4_pair_bf16<3>(o, v.w, scale);
   if (b < nb) *reinterpret_cast<uint32_t*>(q + (r * nb + b) * 16 + 4 * part) = o;
-  if (part == 0) {
+  // the four even (odd) blocks' bytes in every lane of an even (odd) block
+  uint32_t bytes = b < nb ? e8 << (8 * ((b & 7) >> 1)) : 0u;
+  bytes |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(bytes), 8, 64));
+  bytes |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(bytes), 16, 64));
+  const int slot = part + 4 * ((b >> 1) & 3), odd = b & 1;  // 16 lanes of each parity
+  const int64_t kg = b >> 3;
+  if constexpr (SCATTER) {
+    if (slot < sc.k) {
+      const int64_t p = sc.dst[r * sc.k + slot];
+      if (p >= 0) {
+        *reinterpret_cast<uint32_t*>(s + (kg * sc.cap + p) * 8 + 4 * odd) = bytes;
+        if (kg == 0 && odd == 0) sc.tok[p] = static_cast<int32_t>(r);
+      }
+    }
+  } else if (slot == 0) {
     const int64_t batch = r / rows, rr = r - batch * rows;
-    s[((batch * nkg + (b >> 3)) * rows + rr) * 8 + mx_pos(b)] = b < nb ? static_cast<uint8_t>(e8) : 0;
+    *reinterpret_cast<uint32_t*>(s + ((batch * nkg + kg) * rows + rr) * 8 + 4 * odd) = bytes;
   }
 }
 
@@ -214,27 +276,42 @@ hipError_t run_mx(const MxArgs& a, bool small, int kid, hipStream_t s) {
 
 }  // namespace
 
+namespace {
+// scatter: the layer's rows (see Scatter), one workgroup more
+hipError_t quantize_rows(const uint16_t* src, int64_t B, int64_t R, int64_t C, uint8_t* q, uint8_t* s,
+                         const Scatter* sc, hipStream_t st) {
+  const int64_t units = 32 * kgroups(C);  // of 8 values, the last scales' padding included
+  auto go = [&](auto W, auto SC) {
+    mx_quant_kernel<W, SC><<<dim3(static_cast<unsigned>(ceil_div(B * R, 256 / W) + (SC ? 1 : 0)),
+                                  static_cast<unsigned>(ceil_div(units, W))),
+                             256, 0, st>>>(src, B * R, R, static_cast<int>(C), q, s, SC ? *sc : Scatter{});
+  };
+  auto width = [&](auto SC) {
+    if (units <= 32) go(std::integral_constant<int, 32>{}, SC);
+    else if (units <= 64) go(std::integral_constant<int, 64>{}, SC);
+    else go(std::integral_constant<int, 128>{}, SC);
+  };
+  if (sc != nullptr) width(std::true_type{});
+  else width(std::false_type{});
+  return hipGetLastError();
+}
+}  // namespace
+
 hipError_t launch_mx_quantize(const uint16_t* src, int64_t B, int64_t R, int64_t C, int transpose,
                               uint8_t* q, uint8_t* s, hipStream_t st) {
   if (B * R * C == 0) return hipSuccess;
   prof_begin(K_MX_QUANT, st);
+  hipError_t e;
   if (transpose) {
     mx_quant_t_kernel<<<dim3(static_cast<unsigned>(ceil_div(C, 128)), static_cast<unsigned>(kgroups(R)),
                              static_cast<unsigned>(B)),
                         512, 0, st>>>(src, static_cast<int>(R), static_cast<int>(C), q, s);
+    e = hipGetLastError();
   } else {
-    const int64_t units = 32 * kgroups(C);  // of 8 values, the last scales' padding included
-    auto go = [&](auto W) {
-      mx_quant_kernel<W><<<dim3(static_cast<unsigned>(ceil_div(B * R, 256 / W)),
-                                static_cast<unsigned>(ceil_div(units, W))),
-                           256, 0, st>>>(src, B * R, R, static_cast<int>(C), q, s);
-    };
-    if (units <= 32) go(std::integral_constant<int, 32>{});
-    else if (units <= 64) go(std::integral_constant<int, 64>{});
-    else go(std::integral_constant<int, 128>{});
+    e = quantize_rows(src, B, R, C, q, s, nullptr, st);
   }
   prof_end(K_MX_QUANT, st);
-  return hipGetLastError();
+  return e;
 }
 
 hipError_t launch_mx_dequantize(const uint8_t* q, const uint8_t* s, int64_t B, int64_t rows, int64_t K,
@@ -258,6 +335,38 @@ size_t mx_ffn_ws_bytes(int64_t cap, int E_loc, int d, int f, bool indirect) {
   return carve_ffn(nullptr, cap, E_loc, d, f, indirect).bytes;
 }
 
+namespace {
+bool small_tile(int64_t cap, int E_loc, int d, int f) { return cap <= 128 * int64_t{E_loc}; }
+
+// The two products.  xs: the scales of the permuted rows ([..][s_rows][8]);
+// tok: their rows of xq (null: the same); w.mt: the table of row tiles.
+hipError_t products(const uint8_t* xq, int64_t x_rows, const uint8_t* xs, int64_t s_rows, const int32_t* tok,
+                    const FfnWs& w, const int32_t* offsets, int E_loc, int64_t cap, int d, int f,
+                    const uint8_t* const wq[3], const uint8_t* const wsc[3], uint16_t* y, hipStream_t s) {
+  const bool small = small_tile(cap, E_loc, d, f);
+  const int S = small ? TILE_S : TILE;
+  MxArgs a{};
+  a.a = {xq, xs};
+  a.a_tok = tok;
+  a.a_rows = s_rows;
+  a.a_bytes = x_rows * kq_of(d);
+  a.b0 = {wq[0], wsc[0]};
+  a.b1 = {wq[1], wsc[1]};
+  a.act_q = w.act_q; a.act_s = w.act_s; a.cap = cap; a.y = y;
+  a.t.offsets = offsets; a.t.mt_start = w.mt;
+  a.t.E_loc = E_loc; a.t.d = d; a.t.f = f;
+  a.t.NT = static_cast<int>(ceil_div(f, S / 2));
+  if (hipError_t e = run_mx<MX_GATE_UP>(a, small, K_MX_GATE_UP, s); e != hipSuccess) return e;
+  a.a = {w.act_q, w.act_s};
+  a.a_tok = nullptr;
+  a.a_rows = cap;
+  a.a_bytes = cap * kq_of(f);
+  a.b0 = {wq[2], wsc[2]};
+  a.t.NT = static_cast<int>(ceil_div(d, S));
+  return run_mx<MX_DOWN>(a, small, K_MX_DOWN, s);
+}
+}  // namespace
+
 hipError_t launch_mx_ffn(const uint8_t* xq, const uint8_t* xs, int64_t x_rows, const int32_t* row_src,
                          int k, const int32_t* offsets, int E_loc, int64_t cap, int d, int f,
                          const uint8_t* const wq[3], const uint8_t* const wsc[3], uint16_t* y,
@@ -273,35 +382,19 @@ hipError_t launch_mx_ffn(const uint8_t* xq, const uint8_t* xs, int64_t x_rows, c
     prof_end(K_MX_QUANT, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  const bool small = cap <= 128 * int64_t{E_loc};
-  const int S = small ? TILE_S : TILE;
-  if (hipError_t e = launch_gemm_sched(offsets, E_loc, S, BK, w.mt, w.wk, w.nz, s); e != hipSuccess) return e;
-  MxArgs a{};
-  a.a = {xq, indirect ? w.s_perm : xs};
-  a.a_tok = indirect ? w.tok : nullptr;
-  a.a_rows = indirect ? cap : x_rows;
-  a.a_bytes = x_rows * kq_of(d);
-  a.b0 = {wq[0], wsc[0]};
-  a.b1 = {wq[1], wsc[1]};
-  a.act_q = w.act_q; a.act_s = w.act_s; a.cap = cap; a.y = y;
-  a.t.offsets = offsets; a.t.mt_start = w.mt; a.t.wk_start = w.wk; a.t.nz_start = w.nz;
-  a.t.E_loc = E_loc; a.t.d = d; a.t.f = f;
-  a.t.NT = static_cast<int>(ceil_div(f, S / 2));
-  if (hipError_t e = run_mx<MX_GATE_UP>(a, small, K_MX_GATE_UP, s); e != hipSuccess) return e;
-  a.a = {w.act_q, w.act_s};
-  a.a_tok = nullptr;
-  a.a_rows = cap;
-  a.a_bytes = cap * kq_of(f);
-  a.b0 = {wq[2], wsc[2]};
-  a.t.NT = static_cast<int>(ceil_div(d, S));
-  return run_mx<MX_DOWN>(a, small, K_MX_DOWN, s);
+  if (hipError_t e = launch_gemm_sched(offsets, E_loc, small_tile(cap, E_loc, d, f) ? TILE_S : TILE, BK,
+                                       w.mt, w.wk, w.nz, s);
+      e != hipSuccess)
+    return e;
+  return indirect ? products(xq, x_rows, w.s_perm, cap, w.tok, w, offsets, E_loc, cap, d, f, wq, wsc, y, s)
+                  : products(xq, x_rows, xs, x_rows, nullptr, w, offsets, E_loc, cap, d, f, wq, wsc, y, s);
 }
 
 namespace {
 struct LayerWs {
   int32_t *offsets, *row_src, *dst;
   void *perm, *ffn;
-  uint8_t *xq, *xs;
+  uint8_t* xq;
   uint16_t* y_perm;
   size_t bytes;
 };
@@ -320,7 +413,6 @@ LayerWs carve_layer(void* ws, int64_t T, int E, int k, int E_loc, int d, int f) 
   w.dst = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * static_cast<size_t>(T) * k));
   w.perm = take(permute_ws_bytes(T, E, k, E_loc));
   w.xq = reinterpret_cast<uint8_t*>(take(static_cast<size_t>(T) * kq_of(d)));
-  w.xs = reinterpret_cast<uint8_t*>(take(static_cast<size_t>(T) * 8 * kgroups(d)));
   w.y_perm = reinterpret_cast<uint16_t*>(take(sizeof(uint16_t) * static_cast<size_t>(cap) * d));
   w.ffn = take(mx_ffn_ws_bytes(cap, E_loc, d, f, true));
   w.bytes = used;
@@ -342,11 +434,17 @@ hipError_t launch_mx_layer(const uint16_t* x, const int32_t* idx, const float* g
                                     w.dst, nullptr, w.perm, s);
       e != hipSuccess)
     return e;
-  if (hipError_t e = launch_mx_quantize(x, 1, T, d, 0, w.xq, w.xs, s); e != hipSuccess) return e;
-  if (hipError_t e = launch_mx_ffn(w.xq, w.xs, T, w.row_src, k, w.offsets, E_loc, cap, d, f, wq, wsc,
-                                   w.y_perm, w.ffn, s);
-      e != hipSuccess)
-    return e;
+  const FfnWs fw = carve_ffn(w.ffn, cap, E_loc, d, f, true);
+  const Scatter sc{w.dst, w.offsets, fw.tok, fw.mt, cap, k, E_loc,
+                   small_tile(cap, E_loc, d, f) ? TILE_S : TILE};
+  prof_begin(K_MX_QUANT, s);
+  const hipError_t e = quantize_rows(x, 1, T, d, w.xq, fw.s_perm, &sc, s);
+  prof_end(K_MX_QUANT, s);
+  if (e != hipSuccess) return e;
+  if (hipError_t e2 = products(w.xq, T, fw.s_perm, cap, fw.tok, fw, w.offsets, E_loc, cap, d, f, wq, wsc,
+                               w.y_perm, s);
+      e2 != hipSuccess)
+    return e2;
   return launch_combine(w.y_perm, w.dst, gate, T, d, k, y, s);
 }
 

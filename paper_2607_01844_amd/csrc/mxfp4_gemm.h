@@ -145,6 +145,12 @@ struct MxStream {
   }
 };
 
+// Lanes below 32 get the pair (a of their own, a of lane + 32), the others (b of
+// lane - 32, b of their own).
+__device__ __forceinline__ uint2 swap_halves(uint32_t a, uint32_t b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  return make_uint2(r[0], r[1]);
+}
 // Accumulators that have to be there at this point: keeps the matrix
 // instructions before it from being moved behind the branches that follow.
 __device__ __forceinline__ void pin(f32x16& v) { asm volatile("" : "+v"(v)); }
@@ -444,7 +450,10 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
           a[r] = z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)) * acc[i][1][r];
           top = max(top, __float_as_uint(a[r]) & 0x7fffffffu);
         }
-        top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), 32, 64)));
+        {
+          const uint2 t = swap_halves(top, top);
+          top = max(t.x, t.y);
+        }
         const uint32_t e8 = mx_scale(top);
         const float sc = __uint_as_float(e8 << 23);
         uint32_t p[2];  // 16 bits of each of two q
@@ -457,20 +466,22 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
           v = fp4_pair<3>(v, a[8 * h + 6], a[8 * h + 7], sc);
           p[h] = v;
         }
-        const uint32_t o0 = static_cast<uint32_t>(__shfl_xor(static_cast<int>(p[0]), 32, 64));
-        const uint32_t o1 = static_cast<uint32_t>(__shfl_xor(static_cast<int>(p[1]), 32, 64));
+        // lanes below 32 end with columns 0 .. 15 of the block (their own and their
+        // partner's 16 bits of two q each), the others with 16 .. 31 of the same row
+        const uint2 c = swap_halves(p[0], p[1]);
         if constexpr (i == 0) wait_vmcnt<0>();  // see front(): loads that the next step reads
         const int rt = rb + l32;
-        if (lh == 0 && rt < mvalid && col < f) {
+        if (rt < mvalid && col < f) {
           const int64_t row = row0 + rt;
           const int fq = (f + 31) / 32 * 16, b = col / 32, nb = (f + 31) / 32;
-          *reinterpret_cast<uint4*>(g.act_q + row * fq + col / 2) =
-              make_uint4((p[0] & 0xffffu) | (o0 << 16), (p[0] >> 16) | (o0 & 0xffff0000u),
-                         (p[1] & 0xffffu) | (o1 << 16), (p[1] >> 16) | (o1 & 0xffff0000u));
-          uint8_t* s = g.act_s + (static_cast<int64_t>(b >> 3) * g.cap + row) * 8;
-          s[mx_pos(b)] = static_cast<uint8_t>(e8);
-          if (b == nb - 1)  // the rest of the last eight, whose values are zeros
-            for (int c = b + 1; (c & 7) != 0; ++c) s[mx_pos(c)] = 0;
+          *reinterpret_cast<uint2*>(g.act_q + row * fq + col / 2 + 8 * lh) =
+              make_uint2((c.x & 0xffffu) | (c.y << 16), (c.x >> 16) | (c.y & 0xffff0000u));
+          if (lh == 0) {
+            uint8_t* s = g.act_s + (static_cast<int64_t>(b >> 3) * g.cap + row) * 8;
+            s[mx_pos(b)] = static_cast<uint8_t>(e8);
+            if (b == nb - 1)  // the rest of the last eight, whose values are zeros
+              for (int z = b + 1; (z & 7) != 0; ++z) s[mx_pos(z)] = 0;
+          }
         }
       } else {
         // through the wave's patch, 16 rows of 64 columns at a time, so that
