@@ -125,22 +125,30 @@ __global__ __launch_bounds__(256) void mx_quant_kernel(const uint16_t* __restric
 }
 
 // Along columns: src [B][K][C] -> q [B][C][kq], s [B][ceil(K / 256)][C][8]: a
-// workgroup takes 256 k of 128 columns, a wave 32 of them (one block a column),
-// a lane two columns; the eight waves' scale bytes leave together.
+// workgroup takes 256 k of TC columns, a wave 32 of them (one block a column), a
+// lane TC / 64 columns; values and scales leave through LDS, a column's 128 bytes
+// together.
+constexpr int TC = 128;
 __global__ __launch_bounds__(512) void mx_quant_t_kernel(const uint16_t* __restrict__ src, int K, int C,
                                                          uint8_t* __restrict__ q,
                                                          uint8_t* __restrict__ s) {
-  __shared__ __align__(8) uint8_t sb[128][8];
+  __shared__ __align__(16) uint4 vb[TC][8];  // 16-byte piece w of column c at w ^ (c / 2 % 8)
+  __shared__ __align__(8) uint8_t sb[TC][8];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int nb = (K + 31) / 32, nkg = (nb + 7) / 8;
-  const int c = blockIdx.x * 128 + 2 * lane;
+  const int c0 = blockIdx.x * TC, c = c0 + 2 * lane;
   const int kg = blockIdx.y, b = kg * 8 + w, k0 = 32 * b;
   const int64_t batch = blockIdx.z;
   const uint16_t* in = src + (batch * K + k0) * C + c;
   uint32_t v[32];
+  if (k0 + 32 <= K && c < C) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-    v[i] = c < C && k0 + i < K ? *reinterpret_cast<const uint32_t*>(in + static_cast<int64_t>(i) * C) : 0u;
+    for (int i = 0; i < 32; ++i) v[i] = *reinterpret_cast<const uint32_t*>(in + static_cast<int64_t>(i) * C);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      v[i] = c < C && k0 + i < K ? *reinterpret_cast<const uint32_t*>(in + static_cast<int64_t>(i) * C) : 0u;
+  }
   uint32_t t0 = 0, t1 = 0;
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
@@ -167,19 +175,25 @@ __global__ __launch_bounds__(512) void mx_quant_t_kernel(const uint16_t* __restr
       r = fp4_pair_bf16<3>(r, x[3], sc);
       o[p] = r;
     }
-    if (b < nb && c < C)
-      *reinterpret_cast<uint4*>(q + ((batch * C + c + h) * nb + b) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+    vb[2 * lane + h][w ^ (lane & 7)] = make_uint4(o[0], o[1], o[2], o[3]);
     sb[2 * lane + h][mx_pos(w)] = b < nb ? static_cast<uint8_t>(e[h]) : 0;
   }
   __syncthreads();
+#pragma unroll
+  for (int i = 0; i < TC / 64; ++i) {
+    const int cc = 64 * i + (threadIdx.x >> 3), piece = threadIdx.x & 7;
+    if (c0 + cc < C && kg * 8 + piece < nb)
+      *reinterpret_cast<uint4*>(q + ((batch * C + c0 + cc) * nb + kg * 8 + piece) * 16) =
+          vb[cc][piece ^ ((cc >> 1) & 7)];
+  }
   const int cc = threadIdx.x;
-  if (cc < 128 && blockIdx.x * 128 + cc < C)
-    *reinterpret_cast<uint2*>(s + ((batch * nkg + kg) * C + blockIdx.x * 128 + cc) * 8) =
-        *reinterpret_cast<const uint2*>(sb[cc]);
+  if (cc < TC && c0 + cc < C)
+    *reinterpret_cast<uint2*>(s + ((batch * nkg + kg) * C + c0 + cc) * 8) = *reinterpret_cast<const uint2*>(sb[cc]);
 }
 
-// dst [rows][K] bf16 of q, s (batches of `rows` rows): 8 values a thread.  Every
-// value is a bf16 (two significant bits, at least 2^-128).
+// dst [rows][K] bf16 of q, s (batches of `rows` rows): 8 values a thread of DR
+// rows.  Every value is a bf16 (two significant bits, at least 2^-128).
+constexpr int DR = 4;
 template <int W>
 __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint8_t* __restrict__ q,
                                                          const uint8_t* __restrict__ s, int64_t total,
@@ -188,28 +202,36 @@ __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint8_t* __restri
   const int nb = (K + 31) / 32, nkg = (nb + 7) / 8;
   const int u = blockIdx.y * W + threadIdx.x % W;
   const int b = u >> 2;
-  const int64_t r = static_cast<int64_t>(blockIdx.x) * RPB + threadIdx.x / W;
-  if (r >= total || 8 * u >= K) return;
-  const int64_t batch = r / rows, rr = r - batch * rows;
-  const uint32_t e8 = s[((batch * nkg + (b >> 3)) * rows + rr) * 8 + mx_pos(b)];
-  const uint32_t v = *reinterpret_cast<const uint32_t*>(q + (r * nb + b) * 16 + 4 * (u & 3));
-  const float nan = __uint_as_float(0x7fc00000u);
-  uint32_t o[4];
+  if (8 * u >= K) return;
+  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * (RPB * DR) + threadIdx.x / W;
+  uint32_t e8[DR], v[DR];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float f[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t c = (v >> (8 * i + 4 * h)) & 15u, m = c & 7u;
-      // 0, 1/2 and (1 + m0 / 2) 2^(m / 2 - 1)
-      const float a = m < 2 ? 0.5f * static_cast<float>(m)
-                            : __uint_as_float(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
-      const float x = ldexpf(a, static_cast<int>(e8) - 127);
-      f[h] = e8 == 255u ? nan : c & 8u ? -x : x;
-    }
-    o[i] = pack_bf16x2(f[0], f[1]);
+  for (int i = 0; i < DR; ++i) {
+    const int64_t r = r0 + i * RPB < total ? r0 + i * RPB : total - 1;
+    const int64_t batch = r / rows, rr = r - batch * rows;
+    e8[i] = s[((batch * nkg + (b >> 3)) * rows + rr) * 8 + mx_pos(b)];
+    v[i] = *reinterpret_cast<const uint32_t*>(q + (r * nb + b) * 16 + 4 * (u & 3));
   }
-  *reinterpret_cast<uint4*>(dst + r * K + 8 * u) = make_uint4(o[0], o[1], o[2], o[3]);
+#pragma unroll
+  for (int i = 0; i < DR; ++i) {
+    const int64_t r = r0 + i * RPB;
+    if (r >= total) return;
+    uint32_t o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float x[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t c = v[i] >> (8 * j + 4 * h), m = c & 7u;
+        // 0, 1/2 and (1 + m0 / 2) 2^(m / 2 - 1)
+        const float a = m < 2 ? 0.5f * static_cast<float>(m)
+                              : __uint_as_float(((126u + (m >> 1)) << 23) | ((m & 1u) << 22));
+        x[h] = __builtin_ldexpf(c & 8u ? -a : a, static_cast<int>(e8[i]) - 127);
+      }
+      o[j] = e8[i] == 255u ? 0x7fc07fc0u : pack_bf16x2(x[0], x[1]);
+    }
+    *reinterpret_cast<uint4*>(dst + r * K + 8 * u) = make_uint4(o[0], o[1], o[2], o[3]);
+  }
 }
 
 // Scales of the permuted rows, and each row's token: s_perm [nkg][cap][8].
@@ -320,7 +342,7 @@ hipError_t launch_mx_dequantize(const uint8_t* q, const uint8_t* s, int64_t B, i
   prof_begin(K_MX_QUANT, st);
   const int64_t units = ceil_div(K, 8);
   auto go = [&](auto W) {
-    mx_dequant_kernel<W><<<dim3(static_cast<unsigned>(ceil_div(B * rows, 256 / W)),
+    mx_dequant_kernel<W><<<dim3(static_cast<unsigned>(ceil_div(B * rows, 256 / W * DR)),
                                 static_cast<unsigned>(ceil_div(units, W))),
                            256, 0, st>>>(q, s, B * rows, rows, static_cast<int>(K), dst);
   };
@@ -336,14 +358,27 @@ size_t mx_ffn_ws_bytes(int64_t cap, int E_loc, int d, int f, bool indirect) {
 }
 
 namespace {
-bool small_tile(int64_t cap, int E_loc, int d, int f) { return cap <= 128 * int64_t{E_loc}; }
+// The 128-row tile for experts of up to 128 rows on average, which fill one of
+// them (64 experts of 16 rows, d = 2048, f = 1408, both products: 65 us against
+// 70 on 256-row tiles; 128 rows 88 against 92; beyond the line 160 rows 113
+// against 101, 128 experts of 512 rows, d = 4096, f = 1536 893 against 719), and
+// where 256-row tiles would use less than two thirds of the CUs (12 experts of
+// 256 rows, d = 520, f = 328: 21 us against 31; 16 of 512, d = 1024, f = 512 26
+// against 33; beyond the line 16 of 1000 40 against 36).
+bool small_tile(int64_t rows, int E_loc, int d, int f) {
+  if (rows <= 128 * int64_t{E_loc}) return true;
+  const int64_t cus = device_cus();
+  const int64_t tiles = (std::min<int64_t>(rows, E_loc) + rows / TILE) *
+                        std::max(ceil_div(f, TILE / 2), ceil_div(d, TILE));
+  return 3 * tiles < 2 * cus * ceil_div(tiles, cus);
+}
 
 // The two products.  xs: the scales of the permuted rows ([..][s_rows][8]);
 // tok: their rows of xq (null: the same); w.mt: the table of row tiles.
 hipError_t products(const uint8_t* xq, int64_t x_rows, const uint8_t* xs, int64_t s_rows, const int32_t* tok,
-                    const FfnWs& w, const int32_t* offsets, int E_loc, int64_t cap, int d, int f,
-                    const uint8_t* const wq[3], const uint8_t* const wsc[3], uint16_t* y, hipStream_t s) {
-  const bool small = small_tile(cap, E_loc, d, f);
+                    const FfnWs& w, bool small, const int32_t* offsets, int E_loc, int64_t cap, int d,
+                    int f, const uint8_t* const wq[3], const uint8_t* const wsc[3], uint16_t* y,
+                    hipStream_t s) {
   const int S = small ? TILE_S : TILE;
   MxArgs a{};
   a.a = {xq, xs};
@@ -382,12 +417,12 @@ hipError_t launch_mx_ffn(const uint8_t* xq, const uint8_t* xs, int64_t x_rows, c
     prof_end(K_MX_QUANT, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  if (hipError_t e = launch_gemm_sched(offsets, E_loc, small_tile(cap, E_loc, d, f) ? TILE_S : TILE, BK,
-                                       w.mt, w.wk, w.nz, s);
+  const bool small = small_tile(cap, E_loc, d, f);  // the host knows the capacity alone
+  if (hipError_t e = launch_gemm_sched(offsets, E_loc, small ? TILE_S : TILE, BK, w.mt, w.wk, w.nz, s);
       e != hipSuccess)
     return e;
-  return indirect ? products(xq, x_rows, w.s_perm, cap, w.tok, w, offsets, E_loc, cap, d, f, wq, wsc, y, s)
-                  : products(xq, x_rows, xs, x_rows, nullptr, w, offsets, E_loc, cap, d, f, wq, wsc, y, s);
+  return products(xq, x_rows, indirect ? w.s_perm : xs, indirect ? cap : x_rows, indirect ? w.tok : nullptr,
+                  w, small, offsets, E_loc, cap, d, f, wq, wsc, y, s);
 }
 
 namespace {
@@ -435,14 +470,14 @@ hipError_t launch_mx_layer(const uint16_t* x, const int32_t* idx, const float* g
       e != hipSuccess)
     return e;
   const FfnWs fw = carve_ffn(w.ffn, cap, E_loc, d, f, true);
-  const Scatter sc{w.dst, w.offsets, fw.tok, fw.mt, cap, k, E_loc,
-                   small_tile(cap, E_loc, d, f) ? TILE_S : TILE};
+  const bool small = small_tile(ceil_div(T * k * E_loc, E), E_loc, d, f);  // rows expected here
+  const Scatter sc{w.dst, w.offsets, fw.tok, fw.mt, cap, k, E_loc, small ? TILE_S : TILE};
   prof_begin(K_MX_QUANT, s);
   const hipError_t e = quantize_rows(x, 1, T, d, w.xq, fw.s_perm, &sc, s);
   prof_end(K_MX_QUANT, s);
   if (e != hipSuccess) return e;
-  if (hipError_t e2 = products(w.xq, T, fw.s_perm, cap, fw.tok, fw, w.offsets, E_loc, cap, d, f, wq, wsc,
-                               w.y_perm, s);
+  if (hipError_t e2 = products(w.xq, T, fw.s_perm, cap, fw.tok, fw, small, w.offsets, E_loc, cap, d, f,
+                               wq, wsc, w.y_perm, s);
       e2 != hipSuccess)
     return e2;
   return launch_combine(w.y_perm, w.dst, gate, T, d, k, y, s);
