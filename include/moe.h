@@ -499,7 +499,8 @@ int moe_vocab_loss_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* 
  * logits are finite or -inf (p_s = 0); NaN and +inf make the row's results NaN.
  * workspace: moe_vocab_distill_workspace_bytes() bytes (serves both calls:
  * moe_vocab_loss's, the teacher's probabilities and entries, and a bit per row
- * and 64 columns).
+ * and 64 columns).  The backward takes blocks together while their logit
+ * gradients stay within 64 MiB (2 N vblock bytes each).
  */
 int moe_vocab_distill_workspace_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K,
                                       size_t* bytes);

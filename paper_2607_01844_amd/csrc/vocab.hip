@@ -267,11 +267,14 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(Teacher q, float it, 
   }
 }
 
-// Backward, once: coef_n = dl_n P_n / tau and dl_n p_s / tau of every slot.
+// Backward, once: coef_n = dl_n P_n / tau, and of each vocabulary entry that a
+// row's slots name the sum of dl_n p_s / tau over them, at the first of them
+// (at: its entry; -1 at the others and at absent slots).
 __global__ __launch_bounds__(256) void distill_coef_kernel(Teacher q, float it, int64_t N, int64_t V,
                                                            const float* __restrict__ dloss,
                                                            float* __restrict__ coef,
-                                                           float* __restrict__ dp) {
+                                                           float* __restrict__ dp,
+                                                           int32_t* __restrict__ at) {
   const int lane = threadIdx.x & 63;
   const int64_t n = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (n >= N) return;
@@ -280,37 +283,53 @@ __global__ __launch_bounds__(256) void distill_coef_kernel(Teacher q, float it, 
   teacher_row(q, it, n, V, lane, id, p, P, plogp);
   const float dl = dloss[n] * it;
   if (lane == 0) coef[n] = dl * P;
+  float sum[DK];
+  bool first[DK];
+#pragma unroll
+  for (int i = 0; i < DK; ++i) {
+    sum[i] = p[i];
+    first[i] = id[i] >= 0;
+  }
+#pragma unroll
+  for (int i2 = 0; i2 < DK; ++i2) {
+    const int m = q.K - 64 * i2 < 64 ? q.K - 64 * i2 : 64;
+    for (int j = 0; j < m; ++j) {  // slot 64 i2 + j against this lane's
+      const int o = __builtin_amdgcn_readlane(id[i2], j);
+      const float op = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(p[i2]), j));
+#pragma unroll
+      for (int i = 0; i < DK; ++i) {
+        const bool same = id[i] == o;
+        const bool before = i2 < i || (i2 == i && j < lane), after = i2 > i || (i2 == i && j > lane);
+        first[i] = first[i] && !(same && before);
+        sum[i] += same && after ? op : 0.0f;
+      }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < DK; ++i) {
     const int j = lane + 64 * i;
-    if (j < q.K) dp[n * q.K + j] = dl * p[i];
+    if (j < q.K) {
+      dp[n * q.K + j] = dl * sum[i];
+      at[n * q.K + j] = first[i] ? id[i] : -1;
+    }
   }
 }
 
 // Backward, per block: G at the slots in its columns, from the forward's logits
-// there: G = coef exp(y / tau - lse) - sum of dl p / tau over the row's slots of
-// that column, one rounding.  Thread = slot; of slots of one column the first
-// writes.
-__global__ __launch_bounds__(256) void distill_slots_kernel(Teacher q, float it, int64_t N,
-                                                            int64_t b0, int vb,
-                                                            const float* __restrict__ coef,
+// there: G = coef exp(y / tau - lse) - dp, one rounding.  Thread = slot.
+__global__ __launch_bounds__(256) void distill_slots_kernel(int K, float it, int64_t N, int64_t b0,
+                                                            int vb, const float* __restrict__ coef,
                                                             const float* __restrict__ dp,
+                                                            const int32_t* __restrict__ at,
                                                             const float* __restrict__ yk,
                                                             const float* __restrict__ lse,
                                                             uint16_t* __restrict__ G, int64_t gp) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (i >= N * q.K) return;
-  const int id = q.ids[i];
+  if (i >= N * K) return;
+  const int id = at[i];
   if (id < b0 || id - b0 >= vb) return;
-  const int64_t n = i / q.K;
-  const int j = static_cast<int>(i - n * q.K);
-  const int32_t* row = q.ids + n * q.K;
-  for (int s = 0; s < j; ++s)
-    if (row[s] == id) return;
-  float a = dp[i];
-  for (int s = j + 1; s < q.K; ++s)
-    if (row[s] == id) a += dp[n * q.K + s];
-  const float c = coef[n];
+  const int64_t n = i / K;
+  const float c = coef[n], a = dp[i];
   const float v = c != 0.0f ? __builtin_fmaf(c, __expf(__builtin_fmaf(yk[i], it, -lse[n])), -a) : -a;
   G[n * gp + (id - b0)] = static_cast<uint16_t>(f32_to_bf16_bits(v));
 }
@@ -427,6 +446,17 @@ namespace {
 int hit_words(int64_t vb) { return static_cast<int>(ceil_div(ceil_div(vb, 64), 32)); }
 int padded_slots(int K) { return static_cast<int>(align_up(static_cast<size_t>(K), 4)); }
 
+// Distillation's backward takes as many of the caller's blocks together as
+// keep the logit gradients within 64 MiB: a block of its own four launches each
+// costs more than it saves where it is small (N = 1000, H = 520, V = 32003 in
+// blocks of 4096, 20 slots, forward and backward: 586 us block by block, 328
+// together; N = 256, H = 128, V = 1000 in blocks of 256 133 us against 57).
+int64_t together(int64_t N, int64_t V, int64_t vblock) {
+  if (vblock >= V) return vblock;
+  const int64_t m = (int64_t{64} << 20) / (2 * std::max<int64_t>(1, N)) / vblock;
+  return m > 1 ? vblock * std::min(m, ceil_div(V, vblock)) : vblock;
+}
+
 // Workspace of a forward that takes `span` columns at once; K slots of a
 // teacher per row (0: the plain loss).
 size_t fwd_bytes(int64_t N, int H, int64_t V, int64_t span, int K) {
@@ -442,6 +472,7 @@ size_t fwd_bytes(int64_t N, int H, int64_t V, int64_t span, int K) {
   return b + 256;
 }
 size_t bwd_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K) {
+  if (K > 0) vblock = together(N, V, vblock);
   vblock = bwd_block(N, H, V, vblock);
   const int64_t vb = std::min(vblock, V);
   const int64_t vbp = align_up(vb, 8);
@@ -452,7 +483,7 @@ size_t bwd_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K) {
     b += align_up(sizeof(uint16_t) * static_cast<size_t>(H) * vbp, 256);  // W
   if (K > 0)
     b += align_up(sizeof(float) * static_cast<size_t>(N), 256) +
-         align_up(sizeof(float) * static_cast<size_t>(N) * K, 256);  // coef, dl p
+         2 * align_up(sizeof(float) * static_cast<size_t>(N) * K, 256);  // coef; dl p, entries
   return b + 256;
 }
 size_t fwd_least(int64_t N, int H, int64_t V, int64_t vblock, int K) {
@@ -592,6 +623,7 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
     voc_zero_bf16_kernel<<<static_cast<unsigned>(ceil_div(nw, 256)), 256, 0, s>>>(dw, nw);
     return hipGetLastError();
   }
+  if (q != nullptr) vblock = together(N, V, vblock);
   vblock = bwd_block(N, H, V, vblock);
   const int64_t vbmax = std::min(vblock, V);
   const int64_t vbpmax = align_up(vbmax, 8);
@@ -610,14 +642,17 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
     p += align_up(sizeof(uint16_t) * static_cast<size_t>(H) * vbpmax, 256);
   }
   float *coef = nullptr, *dp = nullptr;
+  int32_t* at = nullptr;
   const float it = q != nullptr ? 1.0f / q->tau : 1.0f;
   if (q != nullptr) {
     coef = reinterpret_cast<float*>(p);
     p += align_up(sizeof(float) * static_cast<size_t>(N), 256);
     dp = reinterpret_cast<float*>(p);
+    p += align_up(sizeof(float) * static_cast<size_t>(N) * q->K, 256);
+    at = reinterpret_cast<int32_t*>(p);
     prof_begin(K_VOC_TEACHER, s);
     distill_coef_kernel<<<static_cast<unsigned>(ceil_div(N, 4)), 256, 0, s>>>(*q, it, N, V, dloss,
-                                                                              coef, dp);
+                                                                              coef, dp, at);
     prof_end(K_VOC_TEACHER, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
@@ -640,7 +675,7 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
         return e;
       prof_begin(K_VOC_TEACHER, s);
       distill_slots_kernel<<<static_cast<unsigned>(ceil_div(N * q->K, 256)), 256, 0, s>>>(
-          *q, it, N, b0, vb, coef, dp, yk, lse, G, gp);
+          q->K, it, N, b0, vb, coef, dp, at, yk, lse, G, gp);
       prof_end(K_VOC_TEACHER, s);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     } else if (hipError_t e = launch_vocab_grad_mfma(x, wb, ldw, bc0, b0, n, H, vb, target, lse,

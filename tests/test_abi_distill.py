@@ -59,10 +59,13 @@ def test_workspace(lib):
     q = lib.moe_vocab_distill_workspace_bytes
     assert q(4096, 2048, 200000, 16384, 64, ctypes.byref(n)) == 0
     assert lib.moe_vocab_loss_workspace_bytes(4096, 2048, 200000, 16384, ctypes.byref(v)) == 0
-    # beside the plain loss's: a probability of every slot and a factor a row
-    assert v.value + 4 * 4096 * 65 <= n.value <= v.value + 4 * 4096 * 65 + 1024
+    # beside the plain loss's: a probability and an entry of every slot and a factor a row
+    assert v.value + 4 * 4096 * 129 <= n.value <= v.value + 4 * 4096 * 129 + 1024
     assert q(4096, 2048, 400000, 16384, 64, ctypes.byref(v)) == 0
     assert v.value == n.value  # independent of V
+    # few rows: blocks are taken together, within 64 MiB of logit gradients
+    assert q(1000, 520, 32003, 4096, 20, ctypes.byref(n)) == 0
+    assert 2 * 1000 * 32003 <= n.value <= 2 * 1000 * 32008 + 8 * 4 * 1000 * 520 + 2 * 520 * 32008 + (1 << 20)
     assert q(10, 64, 100, 16, 4, ctypes.byref(n)) == 0
     assert bwd(nws=16)(lib) == fwd(nws=16)(lib) == fwd(ws=Z)(lib) == -3
     assert q(10, 64, 100, 16, 0, ctypes.byref(n)) == q(10, 64, 100, 16, 4, None) == -1
