@@ -70,7 +70,7 @@ def _given(t, dtype, name, shape):
     _need(t, dtype, name, len(shape))
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{name} is on {t.device}, not on the current device")
     return t
 
