@@ -12,13 +12,24 @@
 // layout that the quantiser writes: [256 k][row][8], the four even blocks' bytes
 // first, so that lane l (row l % 32, blocks of half l / 32) takes its four
 // sub-steps' scales as one dword and each instruction picks its byte.
-//   Both operands are loaded two steps ahead of the step being computed into
-// two slots each (128 KiB, and 8 KiB of scales): a third slot for the weights,
-// as the bf16 kernel has, does not fit beside the scales.  One barrier a step,
-// before its last sub-step: the next step's values have landed, and the slot
-// just read is free for the step after it.  The loads run on their own walk
-// over the tiles (Loader), so tiles follow one another without a pause in the
-// stream, however short they are.
+//   Both operands have two slots each (128 KiB, and 8 KiB of scales; a third for
+// the weights, as the bf16 kernel has, does not fit beside the scales).  B's
+// fragments of a whole step are read in its first sub-step, so that a barrier frees
+// B's slot there and B is loaded a step and a half ahead of its use; A's slot is
+// free before the last sub-step, whose products run from registers while the
+// next step's first fragments are read.  The loads run on their own walk over
+// the tiles, so tiles follow one another without a pause in the stream, however
+// short they are.
+//   Measured, 128 experts of 512 rows, d = 4096, f = 1536, gate/up: 473 us (565 in
+// a sustained run, when the card lowers its clock) for 1.65e12 operations, 3.5e15 a
+// second.  Parts of the same loop with the rest taken out: the products from
+// registers 226 us more than the 74 that epilogues and tile changes take (48 % of
+// the cycles of the whole kernel; on zeros, at a higher clock, the whole takes
+// 403), the loads 250 more, the fragment reads 90 more.  So it is neither the
+// matrix cores, nor the loads, nor LDS alone, but all three in turn under one power
+// limit: half a step more between A's loads and their use (its rows read half by
+// half), or other orders of the steps over K, changed nothing.  With 16 rows an
+// expert the kernel streams its weights: 196 MB in 29 us, 6.8 TB/s.
 #pragma once
 
 #include "gemm_kernel.h"
@@ -348,14 +359,6 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
 #pragma unroll
   for (int j = 0; j < 2; ++j) brow[j] = DUAL ? j * (S / 2) + wn * 32 : wn * 64 + 32 * j;
   f32x16 acc[AIM][2];
-  auto zero_acc = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < AIM; ++i)
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
-  };
   struct Scales {
     int a[AIM], b[2];
   };
@@ -391,20 +394,24 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
     for (int j = 0; j < 2; ++j)
       c.b[j] = *reinterpret_cast<const __attribute__((address_space(3))) int*>(s + 2 * SUNIT + brow[j] * 8);
   };
-  auto mma1 = [&](const Scales& c, auto SUB, auto T) __attribute__((always_inline)) {
+  // FIRST: the tile's first sub-step, which starts from zero
+  auto mma1 = [&](const Scales& c, auto SUB, auto T, auto FIRST) __attribute__((always_inline)) {
     constexpr int i = T / 2, j = T % 2, p = SUB & 1;
     const i32x8 bv = __builtin_shufflevector(fb[SUB][j], fb[SUB][j], 0, 1, 2, 3, -1, -1, -1, -1);
     const i32x8 av = __builtin_shufflevector(fa[p][i], fa[p][i], 0, 1, 2, 3, -1, -1, -1, -1);
-    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bv, av, acc[i][j], 4, 4, SUB, c.b[j], SUB, c.a[i]);
+    if constexpr (FIRST)
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bv, av, f32x16{}, 4, 4, SUB, c.b[j], SUB, c.a[i]);
+    else
+      acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(bv, av, acc[i][j], 4, 4, SUB, c.b[j], SUB, c.a[i]);
     __builtin_amdgcn_sched_barrier(0);
   };
   // The 2 AI products of sub-step SUB.  Between them go the fragment reads of
   // A's next sub-step (and in sub-step 0 all the rest of B's), spread evenly,
   // and extra() halfway.
-  auto mma_read = [&](const Scales& c, int slot, auto SUB, auto AIC, auto&& extra) __attribute__((always_inline)) {
+  auto mma_read = [&](const Scales& c, int slot, auto SUB, auto AIC, auto FIRST, auto&& extra) __attribute__((always_inline)) {
     constexpr int AI = AIC, n = AI + (SUB == 0 ? 6 : 0);  // reads
     static_for<2 * AI>([&](auto T) {
-      mma1(c, SUB, T);
+      mma1(c, SUB, T, FIRST);
       if constexpr (T == AI) {
         extra();
         __builtin_amdgcn_sched_barrier(0);
@@ -551,7 +558,6 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
   Scales sc, sn;
   int slot = 0;
   auto nothing = []() {};
-  zero_acc();
   while (true) {
     // Sub-steps 0 to 2 of the step in `slot`.  B's fragments of all four are read
     // in sub-step 0 and a barrier then frees B's slot, so that B (the weights,
@@ -562,15 +568,15 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
     // the tile's first step, whose next step was loaded before the epilogue's
     // stores and waited for there, so that its end does not wait for the stores.
     auto front = [&](auto AIC, auto FIRST) __attribute__((always_inline)) {
-      mma_read(sc, slot, std::integral_constant<int, 0>{}, AIC, nothing);
+      mma_read(sc, slot, std::integral_constant<int, 0>{}, AIC, FIRST, nothing);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
-      mma_read(sc, slot, std::integral_constant<int, 1>{}, AIC, [&]() __attribute__((always_inline)) {
+      mma_read(sc, slot, std::integral_constant<int, 1>{}, AIC, std::false_type{}, [&]() __attribute__((always_inline)) {
         load_b(slot);
         load_s(slot);
       });
-      mma_read(sc, slot, std::integral_constant<int, 2>{}, AIC, nothing);
+      mma_read(sc, slot, std::integral_constant<int, 2>{}, AIC, std::false_type{}, nothing);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // this wave's reads of the slot are done
       if constexpr (!FIRST) wait_vmcnt<6>();              // and the next step has landed
       __builtin_amdgcn_s_barrier();
@@ -587,7 +593,7 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
       }
       __builtin_amdgcn_sched_barrier(0);
       static_for<2 * AI>([&](auto T) {
-        mma1(sc, std::integral_constant<int, 3>{}, T);
+        mma1(sc, std::integral_constant<int, 3>{}, T, std::false_type{});
         if constexpr (T == 0) {
           load_a(slot);
           __builtin_amdgcn_sched_barrier(0);
@@ -637,7 +643,6 @@ __global__ __launch_bounds__(MxGeom<S>::NTHR, 2) void mxfp4_gemm_kernel(MxArgs g
     epilogue(tc, ai);
     tc = pop();
     if (!tc.valid) break;
-    zero_acc();
   }
   wait_vmcnt<0>();
 }
