@@ -1121,72 +1121,105 @@ __global__ __launch_bounds__(Geom<S>::NTHR, 2) void grouped_gemm_kernel(GemmArgs
           }
         }
         if constexpr (MODE == VD_FWD) {
-          // Few rows with a slot here (a large vocabulary): one after the other, the
-          // wave loading 64 of the row's slots at once (the next row's meanwhile);
-          // each of the few in these columns has its logit in one lane's
-          // accumulators.  Many (a small one): every lane looks through its own
-          // row's slots, four at a time.  N = 4096, H = 2048, V = 200000, 64 slots:
-          // the product takes 3113 us row by row, 3941 lane by lane, 2970 without
-          // slots; N = 256, H = 128, V = 1000, 8 slots 56 against 15.  A row of the
-          // first way costs about what 5/3 slots of the second do.
+          // Few slots here (a large vocabulary): four rows at a time, the wave loading
+          // each one's slots at once; each of the few in these columns has its
+          // logit in one lane's accumulators.  Many (a small vocabulary, or columns that
+          // most rows' teachers rank high): every lane looks through its own row's
+          // slots, 16 at a time.  Rows (as two) and slots in these columns are
+          // counted as they come, and once they have cost a scan the rest is scanned.
+          // Measured, the whole product: N = 4096, H = 2048, V = 200000, 64 slots 3110 us,
+          // by scans alone 3941, without slots 2970; N = 256, H = 128, V = 1000, 8 slots
+          // 15 us, by rows alone 56; N = 284, H = 304, V = 130687, 113 slots, some columns
+          // in most rows, 205 us, by rows alone 305.
           const bool in = rok && lh == 0 && cb < g.dN;
           const uint32_t word = in ? g.hits[row * g.hw + (cb >> 11)] : 0u;
           uint64_t rows = __ballot(((word >> ((cb >> 6) & 31)) & 1u) != 0);
           const int first = static_cast<int>(g.v0) + cb;
           const int32_t* const base = g.ids + ((int64_t)m0 + rb) * g.Kp;
-          // the logit in this lane's accumulators at column `col` of the 64
+          // The logit in this lane's accumulators at column `col` of the 64 (32 j + 8 p +
+          // 4 half + u), picked bit by bit with 31 bit-selects.  (The masks are
+          // opaque: a choice by a known bit becomes an indexed read, 16 selects each.)
           auto logit = [&](int col) __attribute__((always_inline)) {
-            float val = 0.0f;
+            auto mask = [&](int at) __attribute__((always_inline)) {
+              return static_cast<uint32_t>(opaque(-((col >> at) & 1)));
+            };
+            const uint32_t u0 = mask(0), u1 = mask(1), p0 = mask(3), p1 = mask(4), mj = mask(5);
+            auto pick = [](uint32_t m, uint32_t one, uint32_t zero) __attribute__((always_inline)) {
+              return (one & m) | (zero & ~m);
+            };
+            uint32_t of[2];
             static_for<2>([&](auto J) {
-              static_for<16>([&](auto R) {
-                constexpr int j = J, e = R;
-                // a sum of selects (one term matches): the compiler keeps
-                // it in registers instead of indexing the accumulators
-                val += (col & ~4) == 32 * j + 8 * (e / 4) + (e % 4) ? acc[i][j][e] : 0.0f;
+              constexpr int j = J;
+              uint32_t v[4];
+              static_for<4>([&](auto P) {
+                constexpr int e = 4 * P;
+                auto bits = [&](auto U) __attribute__((always_inline)) { return __float_as_uint(acc[i][j][e + U]); };
+                v[P] = pick(u1, pick(u0, bits(std::integral_constant<int, 3>{}), bits(std::integral_constant<int, 2>{})),
+                            pick(u0, bits(std::integral_constant<int, 1>{}), bits(std::integral_constant<int, 0>{})));
               });
+              of[j] = pick(p1, pick(p0, v[3], v[2]), pick(p0, v[1], v[0]));
             });
-            return val;
+            return __uint_as_float(pick(mj, of[1], of[0]));
           };
-          if (5 * __builtin_popcountll(rows) > 3 * g.Kp) {
+          auto here = [&](int id) __attribute__((always_inline)) {
+            const int c = id - first;
+            return id >= 0 && c >= 0 && c < 64 && cb + c < g.dN;
+          };
+          int budget = g.Kp + 8;
+          if (3 * __builtin_popcountll(rows) > budget) budget = 0;
+          while (rows != 0 && budget > 0) {
+            int r[4];
+            int4 q[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              r[u] = rows != 0 ? static_cast<int>(__builtin_ctzll(rows)) : -1;
+              rows &= rows - 1;
+              q[u] = make_int4(-1, -1, -1, -1);
+              if (r[u] >= 0 && 4 * lane < g.Kp)
+                q[u] = *reinterpret_cast<const int4*>(base + (int64_t)r[u] * g.Kp + 4 * lane);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int id4[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+              budget -= 2;
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                uint64_t hit = __ballot(here(id4[t]));
+                budget -= static_cast<int>(__builtin_popcountll(hit));
+                while (hit != 0) {
+                  const int at = __builtin_ctzll(hit);
+                  hit &= hit - 1;
+                  const int col = __builtin_amdgcn_readlane(id4[t], at) - first;
+                  const float val = logit(col);
+                  if (lane == r[u] + 32 * ((col >> 2) & 1))
+                    g.yk[((int64_t)m0 + rb + r[u]) * g.K + 4 * at + t] = val;
+                }
+              }
+            }
+          }
+          if (rows != 0) {
             const bool has = rok && ((rows >> l32) & 1) != 0;
-            for (int s = 0; s < g.Kp; s += 4) {
-              int4 q = make_int4(-1, -1, -1, -1);
-              if (has) q = *reinterpret_cast<const int4*>(base + (int64_t)l32 * g.Kp + s);
-              const int id4[4] = {q.x, q.y, q.z, q.w};
+            for (int s = 0; s < g.Kp; s += 16) {
+              int4 q[4];
 #pragma unroll
               for (int u = 0; u < 4; ++u) {
-                const int c = id4[u] - first;
-                const bool hit = id4[u] >= 0 && c >= 0 && c < 64 && cb + c < g.dN && ((c >> 2) & 1) == lh;
-                if (!__any(hit)) continue;
-                const float val = logit(c);
-                if (hit) g.yk[row * g.K + s + u] = val;
+                q[u] = make_int4(-1, -1, -1, -1);
+                if (has && s + 4 * u < g.Kp)
+                  q[u] = *reinterpret_cast<const int4*>(base + (int64_t)l32 * g.Kp + s + 4 * u);
+              }
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                const int id4[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                  const int c = id4[t] - first;
+                  const bool hit = here(id4[t]) && ((c >> 2) & 1) == lh;
+                  if (!__any(hit)) continue;
+                  const float val = logit(c);
+                  if (hit) g.yk[row * g.K + s + 4 * u + t] = val;
+                }
               }
             }
-            rows = 0;
-          }
-          auto slots = [&](uint64_t of, int s) __attribute__((always_inline)) {  // of the first row in `of`
-            const int r = of != 0 ? __builtin_ctzll(of) : 0;
-            return of != 0 && s + lane < g.K ? base[(int64_t)r * g.Kp + s + lane] : -1;
-          };
-          int id = slots(rows, 0);
-          while (rows != 0) {
-            const int r = __builtin_ctzll(rows);
-            const uint64_t left = rows & (rows - 1);
-            const int ahead = slots(left, 0);
-            for (int s = 0; s < g.K; s += 64) {
-              if (s > 0) id = slots(rows, s);
-              const int c = id - first;
-              uint64_t hit = __ballot(id >= 0 && c >= 0 && c < 64 && cb + c < g.dN);
-              while (hit != 0) {
-                const int q = __builtin_ctzll(hit);
-                hit &= hit - 1;
-                const int col = __builtin_amdgcn_readlane(c, q);  // 32 j + 8 p + 4 half + u
-                const float val = logit(col);
-                if (lane == r + 32 * ((col >> 2) & 1)) g.yk[((int64_t)m0 + rb + r) * g.K + s + q] = val;
-              }
-            }
-            rows = left;
-            id = ahead;
           }
         }
       } else if constexpr (MODE == RT_DX || MODE == VOC_DX) {
