@@ -438,14 +438,16 @@ int64_t bwd_block(int64_t N, int H, int64_t V, int64_t vblock) {
 // K ranges of the dX product: enough (row tile x column tile x range) work
 // items for about two per compute unit of a 256-CU device, each range at
 // least 512 columns (a multiple of 64).  At most 8, and more only of
-// distillation (the loss keeps the order of its sums): as many as stay on the
-// 128-row tile, whose four times as many items then fill the chip (N = 4, H = 616,
-// V = 70554: 17 us, in 8 ranges 87; twice as many ranges, on the 256-row tile, with N =
-// 1, H = 3792, V = 77664 155 us against 105).
-int64_t dx_kspan(int64_t N, int H, int64_t vblock, int K) {
+// distillation (the loss keeps the order of its sums) with few tokens: as many
+// as stay on the 128-row tile, whose four times as many items then fill the chip,
+// and whose partial sums are fewer bytes than W (N = 4, H = 616, V = 70554: 20 us, in
+// 8 ranges 87; twice as many ranges, on the 256-row tile, with N = 1, H = 3792, V =
+// 77664 155 us against 105).
+int64_t dx_kspan(int64_t N, int H, int64_t V, int64_t vblock, int K) {
+  if (K > 0) vblock = std::min(vblock, V);
   const int64_t tiles = std::max<int64_t>(1, ceil_div(N, 256) * ceil_div(H, 256));
   int64_t S = std::min<int64_t>(8, std::max<int64_t>(1, ceil_div(512, tiles)));
-  if (K > 0) S = std::max<int64_t>(S, 2 * 256 / 3 / tiles);
+  if (K > 0) S = std::max<int64_t>(S, std::min<int64_t>(2 * 256 / 3 / tiles, vblock / (4 * std::max<int64_t>(N, 1))));
   S = std::max<int64_t>(1, std::min<int64_t>(S, vblock / 512));
   return align_up(static_cast<size_t>(ceil_div(vblock, S)), 64);
 }
@@ -487,7 +489,7 @@ size_t bwd_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K) {
   vblock = bwd_block(N, H, V, vblock);
   const int64_t vb = std::min(vblock, V);
   const int64_t vbp = align_up(vb, 8);
-  const int64_t slabs = ceil_div(vb, dx_kspan(N, H, vblock, K));
+  const int64_t slabs = ceil_div(vb, dx_kspan(N, H, V, vblock, K));
   size_t b = align_up(sizeof(uint16_t) * static_cast<size_t>(N) * vbp, 256);            // G
   b += align_up(sizeof(float) * static_cast<size_t>(slabs) * N * H, 256);                // dX slabs
   if (staged_bwd(H, V, vblock))
@@ -640,7 +642,8 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
   const int64_t vbpmax = align_up(vbmax, 8);
   // a range longer than the block is the block (vblock itself may exceed an int)
   const int kspan = static_cast<int>(
-      std::min<int64_t>(dx_kspan(N, H, vblock, q != nullptr ? q->K : 0), static_cast<int64_t>(align_up(vbmax, 64))));
+      std::min<int64_t>(dx_kspan(N, H, V, vblock, q != nullptr ? q->K : 0),
+                        static_cast<int64_t>(align_up(vbmax, 64))));
   const int slabs = static_cast<int>(ceil_div(vbmax, kspan));  // the first block fills them all
   char* p = static_cast<char*>(ws);
   uint16_t* G = reinterpret_cast<uint16_t*>(p);
