@@ -9,7 +9,10 @@
 // that rule over all bf16 values at scales from 2^-127 to 2^127).  A block with
 // a NaN or an infinity has the scale byte 255, and stands for NaN.
 // The quantisers read each value once, 16 bytes (along rows) or 4 (along
-// columns) a lane, and are bound by that stream.
+// columns) a lane, and are bound by that stream: 64 matrices of 2048 x 1408 (369 MB)
+// along columns 92 to 129 us with 98 MB written, back to bf16 92 to 105, where a copy
+// of the same bytes takes 94; 1100 x 520 along rows 3.1 and 4.3 us, launches.
+// (Twice the bytes a lane along columns is no faster.)
 #include <algorithm>
 
 #include "mxfp4_gemm.h"

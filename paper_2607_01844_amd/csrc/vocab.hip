@@ -437,18 +437,19 @@ int64_t bwd_block(int64_t N, int H, int64_t V, int64_t vblock) {
 
 // K ranges of the dX product: enough (row tile x column tile x range) work
 // items for about two per compute unit of a 256-CU device, each range at
-// least 512 columns (a multiple of 64).  At most 8, and more only of
-// distillation (the loss keeps the order of its sums) with few tokens: as many
-// as stay on the 128-row tile, whose four times as many items then fill the chip,
-// and whose partial sums are fewer bytes than W (N = 4, H = 616, V = 70554: 20 us, in
-// 8 ranges 87; twice as many ranges, on the 256-row tile, with N = 1, H = 3792, V =
-// 77664 155 us against 105).
+// least 512 columns (a multiple of 64; distillation's about 512).  At most 8,
+// and more only of distillation (the loss keeps the order of its sums) with few
+// tokens: as many as stay on the 128-row tile, whose four times as many items
+// then fill the chip, and whose partial sums are fewer bytes than W (N = 4, H =
+// 616, V = 70554: 20 us, in 8 ranges 87; twice as many ranges, on the 256-row tile,
+// with N = 1, H = 3792, V = 77664 155 us against 105).
 int64_t dx_kspan(int64_t N, int H, int64_t V, int64_t vblock, int K) {
   if (K > 0) vblock = std::min(vblock, V);
   const int64_t tiles = std::max<int64_t>(1, ceil_div(N, 256) * ceil_div(H, 256));
   int64_t S = std::min<int64_t>(8, std::max<int64_t>(1, ceil_div(512, tiles)));
-  if (K > 0) S = std::max<int64_t>(S, std::min<int64_t>(2 * 256 / 3 / tiles, vblock / (4 * std::max<int64_t>(N, 1))));
-  S = std::max<int64_t>(1, std::min<int64_t>(S, vblock / 512));
+  if (K > 0)
+    S = std::max<int64_t>(S, std::min<int64_t>(2 * 256 / 3 / tiles, vblock / (4 * std::max<int64_t>(N, 1))));
+  S = std::max<int64_t>(1, std::min<int64_t>(S, K > 0 ? ceil_div(vblock, 512) : vblock / 512));
   return align_up(static_cast<size_t>(ceil_div(vblock, S)), 64);
 }
 
