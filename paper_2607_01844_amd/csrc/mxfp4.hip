@@ -362,11 +362,11 @@ size_t mx_ffn_ws_bytes(int64_t cap, int E_loc, int d, int f, bool indirect) {
 
 namespace {
 // The 128-row tile for experts of up to 128 rows on average, which fill one of
-// them (64 experts of 16 rows, d = 2048, f = 1408, both products: 65 us against
-// 70 on 256-row tiles; 128 rows 88 against 92; beyond the line 160 rows 113
-// against 101, 128 experts of 512 rows, d = 4096, f = 1536 893 against 719), and
+// them (64 experts of 16 rows, d = 2048, f = 1408, both products: 64 us against
+// 69 on 256-row tiles; 128 rows 89 against 91; beyond the line 160 rows 117
+// against 97, 128 experts of 512 rows, d = 4096, f = 1536 884 against 705), and
 // where 256-row tiles would use less than two thirds of the CUs (12 experts of
-// 256 rows, d = 520, f = 328: 21 us against 31; 16 of 512, d = 1024, f = 512 26
+// 256 rows, d = 520, f = 328: 21 us against 30; 16 of 512, d = 1024, f = 512 27
 // against 33; beyond the line 16 of 1000 40 against 36).
 bool small_tile(int64_t rows, int E_loc, int d, int f) {
   if (rows <= 128 * int64_t{E_loc}) return true;

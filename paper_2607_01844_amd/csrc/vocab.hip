@@ -463,8 +463,8 @@ int padded_slots(int K) { return static_cast<int>(align_up(static_cast<size_t>(K
 // Distillation's backward takes as many of the caller's blocks together as
 // keep the logit gradients within 64 MiB: a block of its own four launches each
 // costs more than it saves where it is small (N = 1000, H = 520, V = 32003 in
-// blocks of 4096, 20 slots, forward and backward: 586 us block by block, 328
-// together; N = 256, H = 128, V = 1000 in blocks of 256 133 us against 57).
+// blocks of 4096, 20 slots, forward and backward: 523 us block by block, 300
+// together; N = 256, H = 128, V = 1000 in blocks of 256 127 us against 55).
 int64_t together(int64_t N, int64_t V, int64_t vblock) {
   if (vblock >= V) return vblock;
   const int64_t m = (int64_t{64} << 20) / (2 * std::max<int64_t>(1, N)) / vblock;
