@@ -67,12 +67,13 @@ def _need(t, dtype, name, dim=None):
 def _given(t, dtype, name, shape):
     """A tensor argument of exactly this type and shape on the current device
     (kernels run on the current device's current stream)."""
+    if (t is not None and t.dtype is dtype and t.is_cuda and t.shape == shape and
+            t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice()):
+        return t
     _need(t, dtype, name, len(shape))
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is on {t.device}, not on the current device")
-    return t
+    raise ValueError(f"{name} is on {t.device}, not on the current device")
 
 
 def _out(t, dtype, name, shape, device):
@@ -180,8 +181,7 @@ def moe_route_bwd(x, w_router, logits, topk_idx, topk_gate, dgate, renorm=0, dx=
 def _groups(logits, seq_offsets, token_mask):
     """(T, E, G) of a balance loss call, its arguments checked."""
     _need(logits, torch.float32, "logits", 2)
-    T, E = logits.shape
-    _given(logits, torch.float32, "logits", (T, E))
+    T, E = _given(logits, torch.float32, "logits", logits.shape).shape
     G = 1
     if seq_offsets is not None:
         _need(seq_offsets, torch.int32, "seq_offsets", 1)
