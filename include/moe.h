@@ -497,10 +497,12 @@ int moe_vocab_loss_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* 
  * N * K < 2^31, tau within
  * [MOE_DISTILL_MIN_TEMPERATURE, MOE_DISTILL_MAX_TEMPERATURE].  Present slots'
  * logits are finite or -inf (p_s = 0); NaN and +inf make the row's results NaN.
- * workspace: moe_vocab_distill_workspace_bytes() bytes (serves both calls:
- * moe_vocab_loss's, the teacher's probabilities and entries, and a bit per row
- * and 64 columns).  The backward takes blocks together while their logit
- * gradients stay within 64 MiB (2 N vblock bytes each).
+ * workspace: moe_vocab_distill_workspace_bytes() bytes (serves both calls):
+ * moe_vocab_loss's, the teacher's probabilities and entries, a bit per row and
+ * 64 columns, and at most 448 MiB more: the backward takes blocks together
+ * while their logit gradients (2 N bytes a column) stay within 64 MiB and, where
+ * W's rows are not 16-byte aligned or out of reach, a copy of their columns (2 H
+ * bytes each) within 256; partial sums of dx are 128 MiB of it at most.
  */
 int moe_vocab_distill_workspace_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K,
                                       size_t* bytes);

@@ -461,13 +461,20 @@ int hit_words(int64_t vb) { return static_cast<int>(ceil_div(ceil_div(vb, 64), 3
 int padded_slots(int K) { return static_cast<int>(align_up(static_cast<size_t>(K), 4)); }
 
 // Distillation's backward takes as many of the caller's blocks together as
-// keep the logit gradients within 64 MiB: a block of its own four launches each
-// costs more than it saves where it is small (N = 1000, H = 520, V = 32003 in
-// blocks of 4096, 20 slots, forward and backward: 523 us block by block, 300
+// keep the logit gradients within 64 MiB, and the copy of W's columns, where
+// there is one, within 256 (few rows would otherwise take a copy of all of W,
+// whatever the caller's block): a block of its own four launches each costs
+// more than it saves where it is small (forward and backward of N = 1000, H =
+// 520, V = 32003 in blocks of 4096, 20 slots: 523 us block by block, 300
 // together; N = 256, H = 128, V = 1000 in blocks of 256 127 us against 55).
-int64_t together(int64_t N, int64_t V, int64_t vblock) {
+// Copies of at most 64, 128 and 256 MiB and of all of W, N = 64, H = 4096, V =
+// 151669 in blocks of 8192: 3549, 2765, 2333 and 2310 us; N = 1, H = 3792, V =
+// 77663 in blocks of 304: 1600, 1195, 1194 and 1033.
+int64_t together(int64_t N, int H, int64_t V, int64_t vblock) {
   if (vblock >= V) return vblock;
-  const int64_t m = (int64_t{64} << 20) / (2 * std::max<int64_t>(1, N)) / vblock;
+  constexpr int64_t grad = int64_t{64} << 20, copy = int64_t{256} << 20;
+  int64_t m = grad / (2 * std::max<int64_t>(1, N)) / vblock;
+  if (staged_bwd(H, V, m * vblock)) m = std::min(m, copy / (2 * int64_t{H}) / vblock);
   return m > 1 ? vblock * std::min(m, ceil_div(V, vblock)) : vblock;
 }
 
@@ -486,7 +493,7 @@ size_t fwd_bytes(int64_t N, int H, int64_t V, int64_t span, int K) {
   return b + 256;
 }
 size_t bwd_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K) {
-  if (K > 0) vblock = together(N, V, vblock);
+  if (K > 0) vblock = together(N, H, V, vblock);
   vblock = bwd_block(N, H, V, vblock);
   const int64_t vb = std::min(vblock, V);
   const int64_t vbp = align_up(vb, 8);
@@ -637,7 +644,7 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
     voc_zero_bf16_kernel<<<static_cast<unsigned>(ceil_div(nw, 256)), 256, 0, s>>>(dw, nw);
     return hipGetLastError();
   }
-  if (q != nullptr) vblock = together(N, V, vblock);
+  if (q != nullptr) vblock = together(N, H, V, vblock);
   vblock = bwd_block(N, H, V, vblock);
   const int64_t vbmax = std::min(vblock, V);
   const int64_t vbpmax = align_up(vbmax, 8);
