@@ -334,59 +334,69 @@ __global__ __launch_bounds__(256) void distill_slots_kernel(int K, float it, int
   G[n * gp + (id - b0)] = static_cast<uint16_t>(f32_to_bf16_bits(v));
 }
 
+// Workgroups of 256 threads for n items of a kernel that steps over what is
+// beyond its grid: a launch holds less than 2^32 threads, and 2^16 workgroups
+// fill the chip many times over.
+unsigned groups_for(int64_t n) {
+  return static_cast<unsigned>(std::min<int64_t>(ceil_div(n, 256), 1 << 16));
+}
+
 // dx[i] = bf16(sum over slabs b ascending of dxa[b][i]), 8 values per thread
+// and step (n = N H is a multiple of 8)
 __global__ __launch_bounds__(256) void voc_dx_sum_kernel(const float* __restrict__ dxa, int slabs,
                                                          int64_t n, uint16_t* __restrict__ dx) {
-  const int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
-  if (i >= n) return;  // n = N H is a multiple of 8
-  float v[8];
-  {
-    const float4 a = *reinterpret_cast<const float4*>(dxa + i);
-    const float4 b = *reinterpret_cast<const float4*>(dxa + i + 4);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * 256 * 8;
+  for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 8; i < n; i += step) {
+    float v[8];
+    {
+      const float4 a = *reinterpret_cast<const float4*>(dxa + i);
+      const float4 b = *reinterpret_cast<const float4*>(dxa + i + 4);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    }
+    for (int sl = 1; sl < slabs; ++sl) {
+      const float* p = dxa + static_cast<int64_t>(sl) * n + i;
+      const float4 a = *reinterpret_cast<const float4*>(p);
+      const float4 b = *reinterpret_cast<const float4*>(p + 4);
+      v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z;
+      v[7] += b.w;
+    }
+    *reinterpret_cast<uint4*>(dx + i) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                                   pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
   }
-  for (int sl = 1; sl < slabs; ++sl) {
-    const float* p = dxa + static_cast<int64_t>(sl) * n + i;
-    const float4 a = *reinterpret_cast<const float4*>(p);
-    const float4 b = *reinterpret_cast<const float4*>(p + 4);
-    v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z;
-    v[7] += b.w;
-  }
-  *reinterpret_cast<uint4*>(dx + i) = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                                 pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
 }
 
 // wst[h][c] = c < vb ? w[h][v0 + c] : 0 for c < vbp (padded copy of a block),
-// eight columns a thread, read together whatever their alignment (H = 520,
-// V = 32003: 11 us; two bytes at a time 22)
+// eight columns a thread and step, read together whatever their alignment (H =
+// 520, V = 32003: 11 us; two bytes at a time 22)
 __global__ __launch_bounds__(256) void voc_stage_kernel(const uint16_t* __restrict__ w, int64_t V,
                                                         int64_t v0, int vb, int vbp, int H,
                                                         uint16_t* __restrict__ wst) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   const int per = vbp / 8;
-  if (i >= static_cast<int64_t>(H) * per) return;
-  const int64_t h = i / per;
-  const int c = static_cast<int>(i - h * per) * 8;
-  const uint16_t* src = w + h * V + v0 + c;
-  uint32_t p[4];
-  if (c + 8 <= vb) {
-    __builtin_memcpy(p, src, 16);  // one load, of any alignment
-    *reinterpret_cast<uint4*>(wst + i * 8) = make_uint4(p[0], p[1], p[2], p[3]);
-    return;
-  }
+  const int64_t n = static_cast<int64_t>(H) * per;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n;
+       i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t h = i / per;
+    const int c = static_cast<int>(i - h * per) * 8;
+    const uint16_t* src = w + h * V + v0 + c;
+    uint32_t p[4];
+    if (c + 8 <= vb) {
+      __builtin_memcpy(p, src, 16);  // one load, of any alignment
+    } else {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const uint32_t lo = c + 2 * q < vb ? src[2 * q] : 0u;
-    const uint32_t hi = c + 2 * q + 1 < vb ? src[2 * q + 1] : 0u;
-    p[q] = lo | (hi << 16);
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t lo = c + 2 * q < vb ? src[2 * q] : 0u;
+        const uint32_t hi = c + 2 * q + 1 < vb ? src[2 * q + 1] : 0u;
+        p[q] = lo | (hi << 16);
+      }
+    }
+    *reinterpret_cast<uint4*>(wst + i * 8) = make_uint4(p[0], p[1], p[2], p[3]);
   }
-  *reinterpret_cast<uint4*>(wst + i * 8) = make_uint4(p[0], p[1], p[2], p[3]);
 }
 
 hipError_t stage(const uint16_t* w, int64_t V, int64_t v0, int vb, int vbp, int H, uint16_t* wst,
                  hipStream_t s) {
   const int64_t n = static_cast<int64_t>(H) * (vbp / 8);
-  voc_stage_kernel<<<static_cast<unsigned>(ceil_div(n, 256)), 256, 0, s>>>(w, V, v0, vb, vbp, H, wst);
+  voc_stage_kernel<<<groups_for(n), 256, 0, s>>>(w, V, v0, vb, vbp, H, wst);
   return hipGetLastError();
 }
 
@@ -519,14 +529,14 @@ size_t fwd_least(int64_t N, int H, int64_t V, int64_t vblock, int K) {
 // and partly filled last rounds (N = 1000, H = 520, V = 32003 in blocks of
 // 4096: 8 products and merges become 2; N = 4096, H = 2048, V = 200000: 13
 // become 1).  Blocks of fewer than 64 columns stay alone.  A copy of W stays
-// within reach and one launch (2^31 threads of eight columns).
+// within reach.
 int64_t fwd_span(int64_t N, int H, int64_t V, int64_t vblock, int K) {
   const size_t room = std::max(fwd_least(N, H, V, vblock, K), bwd_bytes(N, H, V, vblock, K));
   vblock = fwd_step(H, V, vblock);
   if (vblock % 64 != 0) return vblock;
   int64_t most = std::min<int64_t>(ceil_div(V, vblock), ((int64_t{1} << 40) - 1) / (N * vblock));
   if (staged_fwd(H, V))
-    most = std::min(most, std::min(max_pitch(std::min(H, 32)), (int64_t{1} << 34) / H) / vblock);
+    most = std::min(most, max_pitch(std::min(H, 32)) / vblock);
   int64_t lo = 1, hi = std::max<int64_t>(1, most);  // the largest m in [lo, hi] that fits
   while (lo < hi) {
     const int64_t mid = (lo + hi + 1) / 2;
@@ -643,8 +653,7 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
                    int64_t V, int64_t vblock, uint16_t* dx, uint16_t* dw, void* ws, hipStream_t s) {
   if (N == 0) {  // no tokens: the weight gradient is exact zeros (dx is empty)
     const int64_t nw = static_cast<int64_t>(H) * V;  // H is a multiple of 8
-    const int64_t groups = std::min<int64_t>(ceil_div(nw, 256 * 8), 1 << 20);  // (a launch holds 2^32 threads)
-    voc_zero_bf16_kernel<<<static_cast<unsigned>(groups), 256, 0, s>>>(dw, nw);
+    voc_zero_bf16_kernel<<<groups_for(nw / 8), 256, 0, s>>>(dw, nw);
     return hipGetLastError();
   }
   if (q != nullptr) vblock = together(N, H, V, vblock);
@@ -715,7 +724,7 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
       return e;
   }
   const int64_t nx = N * H;
-  voc_dx_sum_kernel<<<static_cast<unsigned>(ceil_div(nx / 8, 256)), 256, 0, s>>>(dxa, slabs, nx, dx);
+  voc_dx_sum_kernel<<<groups_for(nx / 8), 256, 0, s>>>(dxa, slabs, nx, dx);
   return hipGetLastError();
 }
 
