@@ -560,6 +560,21 @@ size_t distill_bwd_ws_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K) 
 }
 
 namespace {
+// f(first, rows) over the N rows in pieces that a launch of a wave a row holds
+// (less than 2^32 threads).
+template <typename F>
+void by_rows(int64_t N, F&& f) {
+  constexpr int64_t most = int64_t{1} << 25;
+  for (int64_t n0 = 0; n0 < N; n0 += most) f(n0, std::min(most, N - n0));
+}
+// The teacher of the rows from n0 on.
+Teacher from_row(Teacher q, int64_t n0) {
+  q.ids += n0 * q.K;
+  q.t += n0 * q.K;
+  if (q.tlse != nullptr) q.tlse += n0;
+  return q;
+}
+
 // The forward of either loss: against targets, or a teacher (q, yk).
 hipError_t run_fwd(const uint16_t* x, const uint16_t* w, const int32_t* target, const Teacher* q,
                    int64_t N, int H, int64_t V, int64_t vblock, float* loss, float* lse, float* yk,
@@ -614,8 +629,11 @@ hipError_t run_fwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
     if (K > 0) {
       const int hw = hit_words(vb);
       prof_begin(K_VOC_TEACHER, s);
-      distill_prep_kernel<<<static_cast<unsigned>(ceil_div(N, 4)), 256, 0, s>>>(
-          *q, rows.it, N, V, b0, vb, hw, Kp, first, prob, yt, ids, yk, hits);
+      by_rows(N, [&](int64_t n0, int64_t nr) {
+        distill_prep_kernel<<<static_cast<unsigned>(ceil_div(nr, 4)), 256, 0, s>>>(
+            from_row(*q, n0), rows.it, nr, V, b0, vb, hw, Kp, first, prob + n0 * K, yt + n0, ids + n0 * Kp,
+            yk + n0 * K, hits + n0 * hw);
+      });
       prof_end(K_VOC_TEACHER, s);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
       if (hipError_t e = launch_distill_logits_mfma(x, wb, ldw, bc0, b0, n, H, vb, rows.it, hits, hw,
@@ -632,13 +650,16 @@ hipError_t run_fwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
     const float2* pairs = reinterpret_cast<const float2*>(part);
     const int64_t rounds = ceil_div(ceil_div(ng, per), 64 / sub);  // of one wave a row
     auto merge = [&](auto DIST) {
-      const float* at = DIST ? yk : yt;
       if (rounds <= (sub < 64 ? 4 : 1) || N > (int64_t{1} << 23))  // or rows enough
-        voc_merge_kernel<1, DIST><<<static_cast<unsigned>(ceil_div(N, 4)), 256, 0, s>>>(
-            pairs, ng, per, sub, N, m, sm, first, last, at, loss, lse, rows);
+        by_rows(N, [&](int64_t n0, int64_t nr) {
+          voc_merge_kernel<1, DIST><<<static_cast<unsigned>(ceil_div(nr, 4)), 256, 0, s>>>(
+              pairs + n0 * ng, ng, per, sub, nr, m + n0, sm + n0, first, last,
+              DIST ? yk + n0 * K : yt + n0, loss + n0, lse + n0,
+              DistRows{rows.p + n0 * K, rows.plogp + n0, K, rows.it});
+        });
       else
         voc_merge_kernel<4, DIST><<<static_cast<unsigned>(N), 256, 0, s>>>(
-            pairs, ng, per, sub, N, m, sm, first, last, at, loss, lse, rows);
+            pairs, ng, per, sub, N, m, sm, first, last, DIST ? yk : yt, loss, lse, rows);
     };
     if (K > 0) merge(std::true_type{});
     else merge(std::false_type{});
@@ -685,8 +706,10 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
     p += align_up(sizeof(float) * static_cast<size_t>(N) * q->K, 256);
     at = reinterpret_cast<int32_t*>(p);
     prof_begin(K_VOC_TEACHER, s);
-    distill_coef_kernel<<<static_cast<unsigned>(ceil_div(N, 4)), 256, 0, s>>>(*q, it, N, V, dloss,
-                                                                              coef, dp, at);
+    by_rows(N, [&](int64_t n0, int64_t nr) {
+      distill_coef_kernel<<<static_cast<unsigned>(ceil_div(nr, 4)), 256, 0, s>>>(
+          from_row(*q, n0), it, nr, V, dloss + n0, coef + n0, dp + n0 * q->K, at + n0 * q->K);
+    });
     prof_end(K_VOC_TEACHER, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
