@@ -311,9 +311,11 @@ hipError_t quantize_rows(const uint16_t* src, int64_t B, int64_t R, int64_t C, u
                                   static_cast<unsigned>(ceil_div(units, W))),
                              256, 0, st>>>(src, B * R, R, static_cast<int>(C), q, s, SC ? *sc : Scatter{});
   };
+  // two rows a workgroup would pass the 2^32 threads of a launch from 2^25 - 1 rows on
+  const bool many = B * R > int64_t{1} << 24;
   auto width = [&](auto SC) {
     if (units <= 32) go(std::integral_constant<int, 32>{}, SC);
-    else if (units <= 64) go(std::integral_constant<int, 64>{}, SC);
+    else if (units <= 64 || many) go(std::integral_constant<int, 64>{}, SC);
     else go(std::integral_constant<int, 128>{}, SC);
   };
   if (sc != nullptr) width(std::true_type{});
