@@ -576,12 +576,14 @@ MOE_API int moe_mxfp4_bytes(int64_t B, int64_t rows, int K, size_t* q_bytes, siz
 MOE_API int moe_mxfp4_quantize(const moe_bf16* src, int64_t B, int64_t R, int C, int transpose,
                                uint8_t* q, uint8_t* s, void* stream) {
   const char* fn = "moe_mxfp4_quantize";
-  if (int r = check_mx(fn, B, R, C)) return r;
   CHECK(transpose == 0 || transpose == 1, "transpose must be 0 or 1");
-  if (transpose && B * R > 0) {
-    CHECK(R <= MOE_MAX_DIM, "R > MOE_MAX_DIM with transpose");
+  if (transpose && B != 0 && R != 0) {  // matrices of C rows along R
+    CHECK(R >= 0 && R <= MOE_MAX_DIM, "R out of [0, MOE_MAX_DIM] with transpose");
     if (int r = check_dim(fn, static_cast<int>(R), "R")) return r;
-    CHECK(B * C < (int64_t{1} << 25), "B*C >= 2^25 with transpose");
+    if (int r = check_dim(fn, C, "columns")) return r;
+    if (int r = check_mx(fn, B, C, static_cast<int>(R))) return r;
+  } else {
+    if (int r = check_mx(fn, B, R, C)) return r;
   }
   if (B * R > 0) {
     REQ(src); REQ(q); REQ(s);
