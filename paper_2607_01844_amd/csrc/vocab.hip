@@ -44,7 +44,8 @@ struct DistRows {
   float it;  // 1 / tau
 };
 
-// Merge of two (max, sum of exp(y - max)) pairs; an empty pair is (-inf, 0).
+// Merge of two (max, sum of exp(y - max)) pairs; an empty pair is (-inf, 0).  A
+// sum of NaN stays NaN (its maximum is never -inf).
 // The fused add is written out, so that every caller rounds alike.
 __device__ __forceinline__ void lse_merge(float& m, float& s, float m2, float s2) {
   const float mm = fmaxf(m, m2);
