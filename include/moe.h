@@ -496,7 +496,8 @@ int moe_vocab_loss_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* 
  * Limits: those of moe_vocab_loss, N < 2^26, 1 <= K <= MOE_DISTILL_MAX_K,
  * N * K < 2^31, tau within
  * [MOE_DISTILL_MIN_TEMPERATURE, MOE_DISTILL_MAX_TEMPERATURE].  Present slots'
- * logits are finite or -inf (p_s = 0); NaN and +inf make the row's results NaN.
+ * logits over tau are finite in fp32 or -inf (p_s = 0); NaN and +inf make the
+ * row's loss and gradients NaN (so does, in either loss, a NaN logit Y[n][v]).
  * workspace: moe_vocab_distill_workspace_bytes() bytes (serves both calls):
  * moe_vocab_loss's, the teacher's probabilities and entries, a bit per row and
  * 64 columns, and at most 448 MiB more: the backward takes blocks together

@@ -185,6 +185,7 @@ __device__ __forceinline__ void teacher_row(const Teacher& q, float it, int64_t 
     id[i] = j < q.K ? q.ids[n * q.K + j] : -1;
     if (id[i] >= V) id[i] = -1;
     p[i] = id[i] >= 0 ? q.t[n * q.K + j] * it : NEG;
+    if (p[i] == -NEG) p[i] = __builtin_nanf("");  // no probability: the row becomes NaN
     m = fmaxf(m, p[i]);
   }
   float shift;
