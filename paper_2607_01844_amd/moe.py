@@ -723,6 +723,10 @@ def layer_fwd_bwd(inp: dict, k: int, expert_begin=0, num_local=None, renorm=0,
     inp["seq_offsets"] and inp["token_mask"], their means over its sequences
     and without its padding), dx becomes the whole layer's, and dw_router,
     dbias (with a router bias), balance, zloss and expert_counts are returned.
+    With num_local < E experts (an expert-parallel rank, which sees the same
+    tokens as its peers) dx, dw_router and dbias are this rank's terms of sums
+    over the ranks; num_local / E of the two losses' gradient is in each, so
+    that the sums hold it once.  balance and zloss are whole on every rank.
     """
     x = inp["x"]
     E = inp["w_router"].shape[1]
@@ -746,7 +750,7 @@ def layer_fwd_bwd(inp: dict, k: int, expert_begin=0, num_local=None, renorm=0,
         seq, mask = inp.get("seq_offsets"), inp.get("token_mask")
         balance, zloss, counts, _, n = moe_balance_loss_fwd(logits, idx, seq, mask)
         G = n.shape[0]
-        db, dz = (torch.full((G,), c / G, dtype=torch.float32, device=x.device)
+        db, dz = (torch.full((G,), c / G * (num_local / E), dtype=torch.float32, device=x.device)
                   for c in router_loss)
         aux = moe_balance_loss_bwd(logits, counts, n, db, dz, k, seq, mask)
         dwr, dbias, _ = moe_route_bwd(x, inp["w_router"], logits, idx, gate, dgate, renorm, dx=dx,
