@@ -1085,31 +1085,23 @@ __global__ __launch_bounds__(Geom<S>::NTHR, 2) void grouped_gemm_kernel(GemmArgs
         });
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
         if constexpr (MODE == VD_FWD) mx *= g.it;
+        // All -inf, or no column here: the empty pair (-inf, 0), which merges
+        // without a trace.  NaN alone, which the maximum passes over: (0, NaN).
+        const bool none = mx == NEG;
+        mx = none ? 0.0f : mx;
         float sm = 0.0f;
-        if (mx != NEG) {
-          static_for<2>([&](auto J) {
-            static_for<16>([&](auto R) {
-              constexpr int j = J, r = R;
-              const int c = cb + 32 * j + 8 * (r / 4) + 4 * lh + (r % 4);
-              if (c < g.dN) {
-                if constexpr (MODE == VD_FWD) sm += __expf(__builtin_fmaf(acc[i][j][r], g.it, -mx));
-                else sm += __expf(acc[i][j][r] - mx);
-              }
-            });
+        static_for<2>([&](auto J) {
+          static_for<16>([&](auto R) {
+            constexpr int j = J, r = R;
+            const int c = cb + 32 * j + 8 * (r / 4) + 4 * lh + (r % 4);
+            if (c < g.dN) {
+              if constexpr (MODE == VD_FWD) sm += __expf(__builtin_fmaf(acc[i][j][r], g.it, -mx));
+              else sm += __expf(acc[i][j][r] - mx);
+            }
           });
-        } else {
-          // no column here, all logits -inf: the empty pair, which merges without
-          // a trace; or NaN among them, which the maximum passes over: (0, NaN)
-          static_for<2>([&](auto J) {
-            static_for<16>([&](auto R) {
-              constexpr int j = J, r = R;
-              const int c = cb + 32 * j + 8 * (r / 4) + 4 * lh + (r % 4);
-              if (c < g.dN && acc[i][j][r] != acc[i][j][r]) sm = acc[i][j][r];
-            });
-          });
-        }
+        });
         sm += __shfl_xor(sm, 32, 64);
-        if (mx == NEG && sm != sm) mx = 0.0f;
+        if (none && sm == sm) mx = NEG;
         if (rok) {
           const int ng = (g.dN + 63) >> 6;
           if (lh == 0 && cb < g.dN)
