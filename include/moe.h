@@ -37,7 +37,8 @@
  *    kernels address a tile's rows with 32-bit offsets).  Calls outside the
  *    limits return MOE_ERR_INVALID_ARG.
  *  - Device-side garbage (an expert id outside [0, E) in a caller-supplied
- *    topk_idx) is undefined behaviour.
+ *    topk_idx, or one id twice in a token's k of them, whose rows would pass
+ *    cap where num_local < k) is undefined behaviour.
  */
 #ifndef MOE_MI355X_H
 #define MOE_MI355X_H

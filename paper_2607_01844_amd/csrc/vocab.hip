@@ -28,6 +28,14 @@
 // teacher's slots, and the backward's is G = dl / tau P exp(y / tau - lse), the
 // teacher's probabilities being subtracted at its slots (a few of every
 // thousand columns) by a small kernel before the two products.
+//
+// Sums, exponentials and log-sum-exps are fp32.  G is the one value held in fewer
+// bits: rounded to bf16 once (off by 2^-8 of itself at most), as the operand of
+// two bf16 matrix products.  Two bf16 parts would double both products, half of
+// the loss's work.  Many rounded entries average out in dX, and in dW where rows
+// are many; with few rows dW carries the rounding of its few terms whole (error of
+// all results against 64 bits, N = 1000, H = 520, V = 32003: 0.0024 of their
+// norm; rounding the results alone makes 0.0017).
 #include "common.h"
 
 #include <algorithm>

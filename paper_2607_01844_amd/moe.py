@@ -92,7 +92,10 @@ def workspace(nbytes: int, device, tag: str) -> torch.Tensor:
     current stream, tag): calls on one stream are ordered, calls on different
     streams get different buffers.  A buffer replaced by a larger one is
     kept alive until the process ends, so a HIP graph captured with it never
-    replays into freed memory (capture with the sizes it will replay).
+    replays into freed memory (capture with the sizes it will replay).  A graph
+    works in the buffers of the stream it was captured on: graphs captured on one
+    stream (torch.cuda.graph's own, unless it is given another) replay one after
+    the other; to replay two at once, capture each on a stream of its own.
     device: a torch.device, or what names one (text or number)."""
     if type(device) is torch.device and device.type == "cuda":
         index = device.index if device.index is not None else torch.cuda.current_device()
