@@ -493,7 +493,8 @@ int moe_vocab_loss_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* 
  * recomputes each block of logits and writes dx [N][H] = G W_voc^T and
  * dw_voc [H][V] = X^T G in bf16 (fp32 sums; zeros in dw_voc when N = 0) with
  *   G[n][v] = dloss_n / tau ((sum_s p_s) q_n[v] - sum of p_s over slots of v)
- * rounded to bf16 before the two products.  The teacher gets no gradient.
+ * rounded to bf16 before the two products (N <= 64: in two bf16 parts, G to 2^-16
+ * of itself).  The teacher gets no gradient.
  * Limits: those of moe_vocab_loss, N < 2^26, 1 <= K <= MOE_DISTILL_MAX_K,
  * N * K < 2^31, tau within
  * [MOE_DISTILL_MIN_TEMPERATURE, MOE_DISTILL_MAX_TEMPERATURE].  Present slots'
@@ -502,9 +503,10 @@ int moe_vocab_loss_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_t* 
  * workspace: moe_vocab_distill_workspace_bytes() bytes (serves both calls):
  * moe_vocab_loss's, the teacher's probabilities and entries, a bit per row and
  * 64 columns, and at most 448 MiB more: the backward takes blocks together
- * while their logit gradients (2 N bytes a column) stay within 64 MiB and, where
- * W's rows are not 16-byte aligned or out of reach, a copy of their columns (2 H
- * bytes each) within 256; partial sums of dx are 128 MiB of it at most.
+ * while their logit gradients (2 N bytes a column, 4 N where N <= 64) stay
+ * within 64 MiB and, where W's rows are not 16-byte aligned or out of reach, a
+ * copy of their columns (2 H bytes each) within 256; partial sums of dx are 128
+ * MiB of it at most.
  */
 int moe_vocab_distill_workspace_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K,
                                       size_t* bytes);

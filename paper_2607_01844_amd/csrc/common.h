@@ -235,14 +235,16 @@ hipError_t launch_vocab_grad_mfma(const uint16_t* x, const uint16_t* w, int64_t 
                                   hipStream_t s);
 //   distill: the same pairs of y / tau, and yk[n][s] = y[n][ids[n][s]] for
 //     slots in the block (hits: see GemmArgs); G[n][c] = bf16(coef[n]
-//     exp(y / tau - lse[n])), zeros for c in [vb, gp).
+//     exp(y / tau - lse[n])), zeros for c in [vb, gp), and, with low, `low`
+//     elements on the bf16 of what that rounding left.
 hipError_t launch_distill_logits_mfma(const uint16_t* x, const uint16_t* w, int64_t ldw,
                                       int64_t bc0, int64_t v0, int N, int H, int vb, float it,
                                       const uint32_t* hits, int hw, const int32_t* ids, int K,
                                       int Kp, float* part, float* yk, hipStream_t s);
 hipError_t launch_distill_grad_mfma(const uint16_t* x, const uint16_t* w, int64_t ldw, int64_t bc0,
                                     int N, int H, int vb, float it, const float* lse,
-                                    const float* coef, uint16_t* G, int64_t gp, hipStream_t s);
+                                    const float* coef, uint16_t* G, int64_t gp, int64_t low,
+                                    hipStream_t s);
 hipError_t launch_vocab_dx_mfma(const uint16_t* G, int64_t gp, const uint16_t* w, int64_t ldw,
                                 int64_t bc0, int N, int H, int vb, int kspan, int first,
                                 float* dxa, hipStream_t s);

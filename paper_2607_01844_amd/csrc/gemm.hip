@@ -359,13 +359,14 @@ hipError_t launch_distill_logits_mfma(const uint16_t* x, const uint16_t* w, int6
 
 hipError_t launch_distill_grad_mfma(const uint16_t* x, const uint16_t* w, int64_t ldw, int64_t bc0,
                                     int N, int H, int vb, float it, const float* lse,
-                                    const float* coef, uint16_t* G, int64_t gp, hipStream_t s) {
+                                    const float* coef, uint16_t* G, int64_t gp, int64_t low,
+                                    hipStream_t s) {
   GemmArgs a{};
   a.da = x; a.db = w; a.dc = G; a.lse = lse; a.dloss = coef;
-  a.a_ld = H; a.b_ld = ldw; a.c_ld = gp; a.bc0 = bc0;
+  a.a_ld = H; a.b_ld = ldw; a.c_ld = gp; a.c_bstride = low; a.bc0 = bc0;
   a.dM = N; a.dN = vb; a.dK = H; a.kspan = H; a.batches = 1;
   a.it = it;
-  return run_dense<VD_GRAD>(a, K_VOC_GRAD, s);
+  return low != 0 ? run_dense<VD_GRAD_PARTS>(a, K_VOC_GRAD, s) : run_dense<VD_GRAD>(a, K_VOC_GRAD, s);
 }
 
 hipError_t launch_vocab_dx_mfma(const uint16_t* G, int64_t gp, const uint16_t* w, int64_t ldw,

@@ -100,12 +100,15 @@ enum Mode {
   VOC_DX,           // vocabulary: dxa[b] (+)= G_b W_b^T, fp32
   VOC_DW,           // vocabulary: dW[:, block] = X^T G, bf16
   VD_FWD,           // distillation: VOC_FWD of y / tau, and the logits at the teacher's slots
-  VD_GRAD           // distillation: G = bf16(c exp(y / tau - lse))
+  VD_GRAD,          // distillation: G = bf16(c exp(y / tau - lse))
+  VD_GRAD_PARTS     // and, c_bstride elements on, the bf16 of what the rounding left (a mode
+                    // of its own: VD_GRAD has no registers left for it)
 };
 
 template <int MODE>
 struct Traits {
   static constexpr bool DENSE = MODE >= RT_DW;
+  static constexpr bool VDG = MODE == VD_GRAD || MODE == VD_GRAD_PARTS;
   // operand A stored with the output row index contiguous (read transposed)
   static constexpr bool A_N =
       MODE == WGRAD_GATE_UP || MODE == WGRAD_DOWN || MODE == RT_DW || MODE == VOC_DW;
@@ -456,7 +459,7 @@ struct GemmArgs {
   int64_t cc0;              // vocabulary: dW's first column (VOC_DW)
   int dE;                   // router: experts (the lo parts sit 2E columns into DL3)
   int flag;                 // RT_DX: add to dx; VOC_DX: first block (store, no add)
-  // distillation (VD_FWD, VD_GRAD)
+  // distillation (VD_FWD, VD_GRAD, VD_GRAD_PARTS)
   const uint32_t* hits;     // [N][hw]: bit g of a row: it has a slot in columns 64 g .. + 63
   const int32_t* ids;       // [N][Kp]: vocabulary entry of each slot, -1: none
   float* yk;                // [N][K]: logit at each slot
@@ -1309,7 +1312,7 @@ __global__ __launch_bounds__(Geom<S>::NTHR, 2) void grouped_gemm_kernel(GemmArgs
             });
           });
         }
-        if constexpr (MODE == VD_GRAD) {
+        if constexpr (Traits<MODE>::VDG) {
           // G = c exp(y / tau - lse) (0 where c is: a row without slots), 0
           // past the block's columns; the slots' entries are set afterwards
           const int rt = rb + l32;
@@ -1327,41 +1330,54 @@ __global__ __launch_bounds__(Geom<S>::NTHR, 2) void grouped_gemm_kernel(GemmArgs
             });
           });
         }
-        static_for<2>([&](auto J) {
-          static_for<4>([&](auto Q) {
-            constexpr int j = J, q = Q;
-            const int off = l32 * 128 + (((4 * j + q) ^ ((l32 >> 1) & 7)) << 4) + ((lh ^ (l32 >> 4)) & 1) * 8;
-            put8(off, pack4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
+        // the tile's values as bf16 (G: `add` elements on)
+        auto emit = [&](int64_t add) __attribute__((always_inline)) {
+          static_for<2>([&](auto J) {
+            static_for<4>([&](auto Q) {
+              constexpr int j = J, q = Q;
+              const int off = l32 * 128 + (((4 * j + q) ^ ((l32 >> 1) & 7)) << 4) + ((lh ^ (l32 >> 4)) & 1) * 8;
+              put8(off, pack4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
+            });
           });
-        });
-        fence();
-        auto write = [&](auto WHOLE) __attribute__((always_inline)) {
-          static_for<4>([&](auto Tt) {
-            constexpr int t = Tt;
-            const int r = 8 * t + (lane >> 3), c = lane & 7;
-            const uint4 v = unswap(get16(r * 128 + ((c ^ ((r >> 1) & 7)) << 4)), r);
-            const int rt = rb + r, col = n0 + wn * 64 + 8 * c;
-            // column limit: d; the block's columns (VOC_DW); G's whole pitch,
-            // zeros past the block included (VOC_GRAD)
-            const int climit =
-                MODE == VOC_GRAD || MODE == VD_GRAD ? static_cast<int>(g.c_ld) : DENSE ? g.dN : d;
-            if (rt < mvalid && col < climit) {
-              uint16_t* out;
-              if constexpr (MODE == FWD_DOWN) out = g.y + (int64_t)(seg + m0 + rt) * d;
-              else if constexpr (MODE == DGRAD_GATE_UP) out = g.dx + (int64_t)(seg + m0 + rt) * d;
-              else if constexpr (MODE == WGRAD_DOWN) out = g.dwd + e * wdf + (int64_t)(m0 + rt) * d;
-              else if constexpr (MODE == VOC_GRAD || MODE == VD_GRAD) out = static_cast<uint16_t*>(g.dc) + (int64_t)(m0 + rt) * g.c_ld;
-              else out = static_cast<uint16_t*>(g.dc) + (int64_t)(m0 + rt) * g.c_ld + g.cc0;  // VOC_DW
-              if constexpr (MODE == VOC_DW) store_any(out + col, v, g.dN - col);
-              else if constexpr (MODE == FWD_DOWN || MODE == DGRAD_GATE_UP) store_perm<WHOLE>(out + col, v);
-              else *reinterpret_cast<uint4*>(out + col) = v;
-            }
-          });
+          fence();
+          auto write = [&](auto WHOLE) __attribute__((always_inline)) {
+            static_for<4>([&](auto Tt) {
+              constexpr int t = Tt;
+              const int r = 8 * t + (lane >> 3), c = lane & 7;
+              const uint4 v = unswap(get16(r * 128 + ((c ^ ((r >> 1) & 7)) << 4)), r);
+              const int rt = rb + r, col = n0 + wn * 64 + 8 * c;
+              // column limit: d; the block's columns (VOC_DW); G's whole pitch,
+              // zeros past the block included (VOC_GRAD)
+              const int climit =
+                  MODE == VOC_GRAD || Traits<MODE>::VDG ? static_cast<int>(g.c_ld) : DENSE ? g.dN : d;
+              if (rt < mvalid && col < climit) {
+                uint16_t* out;
+                if constexpr (MODE == FWD_DOWN) out = g.y + (int64_t)(seg + m0 + rt) * d;
+                else if constexpr (MODE == DGRAD_GATE_UP) out = g.dx + (int64_t)(seg + m0 + rt) * d;
+                else if constexpr (MODE == WGRAD_DOWN) out = g.dwd + e * wdf + (int64_t)(m0 + rt) * d;
+                else if constexpr (MODE == VOC_GRAD || Traits<MODE>::VDG) out = static_cast<uint16_t*>(g.dc) + add + (int64_t)(m0 + rt) * g.c_ld;
+                else out = static_cast<uint16_t*>(g.dc) + (int64_t)(m0 + rt) * g.c_ld + g.cc0;  // VOC_DW
+                if constexpr (MODE == VOC_DW) store_any(out + col, v, g.dN - col);
+                else if constexpr (MODE == FWD_DOWN || MODE == DGRAD_GATE_UP) store_perm<WHOLE>(out + col, v);
+                else *reinterpret_cast<uint4*>(out + col) = v;
+              }
+            });
+          };
+          if (MODE != FWD_DOWN && MODE != DGRAD_GATE_UP) write(std::false_type{});
+          else if ((d & 63) == 0) write(std::true_type{});
+          else write(std::false_type{});
+          fence();
         };
-        if (MODE != FWD_DOWN && MODE != DGRAD_GATE_UP) write(std::false_type{});
-        else if ((d & 63) == 0) write(std::true_type{});
-        else write(std::false_type{});
-        fence();
+        emit(0);
+        if constexpr (MODE == VD_GRAD_PARTS) {
+          static_for<2>([&](auto J) {
+            static_for<16>([&](auto R) {
+              constexpr int j = J, r = R;
+              acc[i][j][r] -= bf16_to_f32(static_cast<uint16_t>(f32_to_bf16_bits(acc[i][j][r])));
+            });
+          });
+          emit(g.c_bstride);
+        }
       }
     });
   };

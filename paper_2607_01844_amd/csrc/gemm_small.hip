@@ -27,6 +27,7 @@ void launch_small(int mode, unsigned grid, const GemmArgs& a, hipStream_t s) {
     case VOC_DW: return launch<VOC_DW>(grid, a, s);
     case VD_FWD: return launch<VD_FWD>(grid, a, s);
     case VD_GRAD: return launch<VD_GRAD>(grid, a, s);
+    case VD_GRAD_PARTS: return launch<VD_GRAD_PARTS>(grid, a, s);
   }
 }
 

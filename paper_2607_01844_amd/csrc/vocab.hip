@@ -31,11 +31,11 @@
 //
 // Sums, exponentials and log-sum-exps are fp32.  G is the one value held in fewer
 // bits: rounded to bf16 once (off by 2^-8 of itself at most), as the operand of
-// two bf16 matrix products.  Two bf16 parts would double both products, half of
-// the loss's work.  Many rounded entries average out in dX, and in dW where rows
-// are many; with few rows dW carries the rounding of its few terms whole (error of
-// all results against 64 bits, N = 1000, H = 520, V = 32003: 0.0024 of their
-// norm; rounding the results alone makes 0.0017).
+// two bf16 matrix products.  Many rounded entries average out in dX and dW (their
+// errors against 64 bits, N = 1000, H = 520, V = 32003: 0.0024 of their norm;
+// rounding the results alone makes 0.0017).  With few rows the roundings of the
+// few large entries, at the teacher's slots, are all there is (up to 0.0034), so
+// distillation then holds G in two bf16 parts (PARTS_ROWS below).
 #include "common.h"
 
 #include <algorithm>
@@ -279,15 +279,24 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(Teacher q, float it, 
 
 // Backward, once: coef_n = dl_n P_n / tau, and of each vocabulary entry that a
 // row's slots name the sum of dl_n p_s / tau over them, at the first of them
-// (at: its entry; -1 at the others and at absent slots).
+// (at: its entry; -1 at the others and at absent slots).  x2 (few rows, else
+// null): x [N][H] twice, one below the other.
 __global__ __launch_bounds__(256) void distill_coef_kernel(Teacher q, float it, int64_t N, int64_t V,
                                                            const float* __restrict__ dloss,
                                                            float* __restrict__ coef,
                                                            float* __restrict__ dp,
-                                                           int32_t* __restrict__ at) {
+                                                           int32_t* __restrict__ at,
+                                                           const uint16_t* __restrict__ x, int H,
+                                                           uint16_t* __restrict__ x2) {
   const int lane = threadIdx.x & 63;
   const int64_t n = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (n >= N) return;
+  if (x2 != nullptr)
+    for (int h = 8 * lane; h < H; h += 8 * 64) {
+      const uint4 v = *reinterpret_cast<const uint4*>(x + n * H + h);
+      *reinterpret_cast<uint4*>(x2 + n * H + h) = v;
+      *reinterpret_cast<uint4*>(x2 + (N + n) * H + h) = v;
+    }
   int id[DK];
   float p[DK], P, plogp;
   teacher_row(q, it, n, V, lane, id, p, P, plogp);
@@ -326,14 +335,16 @@ __global__ __launch_bounds__(256) void distill_coef_kernel(Teacher q, float it, 
 }
 
 // Backward, per block: G at the slots in its columns, from the forward's logits
-// there: G = coef exp(y / tau - lse) - dp, one rounding.  Thread = slot.
+// there: G = coef exp(y / tau - lse) - dp, one rounding (low: and what it left,
+// `low` elements on).  Thread = slot.
 __global__ __launch_bounds__(256) void distill_slots_kernel(int K, float it, int64_t N, int64_t b0,
                                                             int vb, const float* __restrict__ coef,
                                                             const float* __restrict__ dp,
                                                             const int32_t* __restrict__ at,
                                                             const float* __restrict__ yk,
                                                             const float* __restrict__ lse,
-                                                            uint16_t* __restrict__ G, int64_t gp) {
+                                                            uint16_t* __restrict__ G, int64_t gp,
+                                                            int64_t low) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (i >= N * K) return;
   const int id = at[i];
@@ -341,7 +352,9 @@ __global__ __launch_bounds__(256) void distill_slots_kernel(int K, float it, int
   const int64_t n = i / K;
   const float c = coef[n], a = dp[i];
   const float v = c != 0.0f ? __builtin_fmaf(c, __expf(__builtin_fmaf(yk[i], it, -lse[n])), -a) : -a;
-  G[n * gp + (id - b0)] = static_cast<uint16_t>(f32_to_bf16_bits(v));
+  uint16_t* const to = G + n * gp + (id - b0);
+  *to = static_cast<uint16_t>(f32_to_bf16_bits(v));
+  if (low != 0) to[low] = static_cast<uint16_t>(f32_to_bf16_bits(v - bf16_to_f32(*to)));
 }
 
 // Workgroups of 256 threads for n items of a kernel that steps over what is
@@ -352,7 +365,7 @@ unsigned groups_for(int64_t n) {
 }
 
 // dx[i] = bf16(sum over slabs b ascending of dxa[b][i]), 8 values per thread
-// and step (n = N H is a multiple of 8)
+// and step (n = N H is a multiple of 8), eight slabs' loads in flight at once
 __global__ __launch_bounds__(256) void voc_dx_sum_kernel(const float* __restrict__ dxa, int slabs,
                                                          int64_t n, uint16_t* __restrict__ dx) {
   const int64_t step = static_cast<int64_t>(gridDim.x) * 256 * 8;
@@ -363,6 +376,7 @@ __global__ __launch_bounds__(256) void voc_dx_sum_kernel(const float* __restrict
       const float4 b = *reinterpret_cast<const float4*>(dxa + i + 4);
       v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
     }
+#pragma unroll 8
     for (int sl = 1; sl < slabs; ++sl) {
       const float* p = dxa + static_cast<int64_t>(sl) * n + i;
       const float4 a = *reinterpret_cast<const float4*>(p);
@@ -482,6 +496,17 @@ namespace {
 int hit_words(int64_t vb) { return static_cast<int>(ceil_div(ceil_div(vb, 64), 32)); }
 int padded_slots(int K) { return static_cast<int>(align_up(static_cast<size_t>(K), 4)); }
 
+// Up to how many rows distillation's G is the sum of two bf16 parts (2^-16 of an
+// entry off) held as 2 N rows: dX is a product of 2 N rows whose halves are added
+// with the K ranges' partial sums, dW one over 2 N rows, x twice.  Error of dx and
+// dw against 64 bits over that of rounding the results alone, V = 8000 and 20001,
+// one part, two parts: N = 1 ... 5 up to 1.99, 1.00; 16 1.53, 1.00; 64 1.47, 1.00;
+// 256 1.39.  Forward and backward, H = 1024, V = 50000: N = 64 151 and 178 us; 128
+// 173 and 220; 256 206 and 293 (H = 4096, V = 151669 unaligned, N = 64: 2341 and
+// 2484: with so few rows most of it is W's).
+constexpr int64_t PARTS_ROWS = 64;
+int64_t grad_rows(int64_t N, int K) { return K > 0 && N <= PARTS_ROWS ? 2 * N : N; }
+
 // Distillation's backward takes as many of the caller's blocks together as
 // keep the logit gradients within 64 MiB, and the copy of W's columns, where
 // there is one, within 256 (few rows would otherwise take a copy of all of W,
@@ -492,10 +517,10 @@ int padded_slots(int K) { return static_cast<int>(align_up(static_cast<size_t>(K
 // Copies of at most 64, 128 and 256 MiB and of all of W, N = 64, H = 4096, V =
 // 151669 in blocks of 8192: 3549, 2765, 2333 and 2310 us; N = 1, H = 3792, V =
 // 77663 in blocks of 304: 1600, 1195, 1194 and 1033.
-int64_t together(int64_t N, int H, int64_t V, int64_t vblock) {
+int64_t together(int64_t rows, int H, int64_t V, int64_t vblock) {
   if (vblock >= V) return vblock;
   constexpr int64_t grad = int64_t{64} << 20, copy = int64_t{256} << 20;
-  int64_t m = grad / (2 * std::max<int64_t>(1, N)) / vblock;
+  int64_t m = grad / (2 * std::max<int64_t>(1, rows)) / vblock;
   if (staged_bwd(H, V, m * vblock)) m = std::min(m, copy / (2 * int64_t{H}) / vblock);
   return m > 1 ? vblock * std::min(m, ceil_div(V, vblock)) : vblock;
 }
@@ -515,18 +540,20 @@ size_t fwd_bytes(int64_t N, int H, int64_t V, int64_t span, int K) {
   return b + 256;
 }
 size_t bwd_bytes(int64_t N, int H, int64_t V, int64_t vblock, int K) {
-  if (K > 0) vblock = together(N, H, V, vblock);
-  vblock = bwd_block(N, H, V, vblock);
+  const int64_t rows = grad_rows(N, K);
+  if (K > 0) vblock = together(rows, H, V, vblock);
+  vblock = bwd_block(rows, H, V, vblock);
   const int64_t vb = std::min(vblock, V);
   const int64_t vbp = align_up(vb, 8);
-  const int64_t slabs = ceil_div(vb, dx_kspan(N, H, V, vblock, K));
-  size_t b = align_up(sizeof(uint16_t) * static_cast<size_t>(N) * vbp, 256);            // G
-  b += align_up(sizeof(float) * static_cast<size_t>(slabs) * N * H, 256);                // dX slabs
+  const int64_t slabs = ceil_div(vb, dx_kspan(rows, H, V, vblock, K));
+  size_t b = align_up(sizeof(uint16_t) * static_cast<size_t>(rows) * vbp, 256);         // G
+  b += align_up(sizeof(float) * static_cast<size_t>(slabs) * rows * H, 256);             // dX slabs
   if (staged_bwd(H, V, vblock))
     b += align_up(sizeof(uint16_t) * static_cast<size_t>(H) * vbp, 256);  // W
   if (K > 0)
     b += align_up(sizeof(float) * static_cast<size_t>(N), 256) +
          2 * align_up(sizeof(float) * static_cast<size_t>(N) * K, 256);  // coef; dl p, entries
+  if (rows > N) b += align_up(sizeof(uint16_t) * static_cast<size_t>(rows) * H, 256);  // x twice
   return b + 256;
 }
 size_t fwd_least(int64_t N, int H, int64_t V, int64_t vblock, int K) {
@@ -687,20 +714,21 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
     voc_zero_bf16_kernel<<<groups_for(nw / 8), 256, 0, s>>>(dw, nw);
     return hipGetLastError();
   }
-  if (q != nullptr) vblock = together(N, H, V, vblock);
-  vblock = bwd_block(N, H, V, vblock);
+  const int64_t rows = grad_rows(N, q != nullptr ? q->K : 0);  // of G
+  if (q != nullptr) vblock = together(rows, H, V, vblock);
+  vblock = bwd_block(rows, H, V, vblock);
   const int64_t vbmax = std::min(vblock, V);
   const int64_t vbpmax = align_up(vbmax, 8);
   // a range longer than the block is the block (vblock itself may exceed an int)
   const int kspan = static_cast<int>(
-      std::min<int64_t>(dx_kspan(N, H, V, vblock, q != nullptr ? q->K : 0),
+      std::min<int64_t>(dx_kspan(rows, H, V, vblock, q != nullptr ? q->K : 0),
                         static_cast<int64_t>(align_up(vbmax, 64))));
   const int slabs = static_cast<int>(ceil_div(vbmax, kspan));  // the first block fills them all
   char* p = static_cast<char*>(ws);
   uint16_t* G = reinterpret_cast<uint16_t*>(p);
-  p += align_up(sizeof(uint16_t) * static_cast<size_t>(N) * vbpmax, 256);
+  p += align_up(sizeof(uint16_t) * static_cast<size_t>(rows) * vbpmax, 256);
   float* dxa = reinterpret_cast<float*>(p);
-  p += align_up(sizeof(float) * static_cast<size_t>(slabs) * N * H, 256);
+  p += align_up(sizeof(float) * static_cast<size_t>(slabs) * rows * H, 256);
   uint16_t* wst = nullptr;
   if (staged_bwd(H, V, vblock)) {
     wst = reinterpret_cast<uint16_t*>(p);
@@ -708,6 +736,7 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
   }
   float *coef = nullptr, *dp = nullptr;
   int32_t* at = nullptr;
+  const uint16_t* xg = x;  // x of G's rows
   const float it = q != nullptr ? 1.0f / q->tau : 1.0f;
   if (q != nullptr) {
     coef = reinterpret_cast<float*>(p);
@@ -715,18 +744,21 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
     dp = reinterpret_cast<float*>(p);
     p += align_up(sizeof(float) * static_cast<size_t>(N) * q->K, 256);
     at = reinterpret_cast<int32_t*>(p);
+    p += align_up(sizeof(int32_t) * static_cast<size_t>(N) * q->K, 256);
+    uint16_t* const x2 = rows > N ? reinterpret_cast<uint16_t*>(p) : nullptr;
     prof_begin(K_VOC_TEACHER, s);
     by_rows(N, [&](int64_t n0, int64_t nr) {
       distill_coef_kernel<<<static_cast<unsigned>(ceil_div(nr, 4)), 256, 0, s>>>(
-          from_row(*q, n0), it, nr, V, dloss + n0, coef + n0, dp + n0 * q->K, at + n0 * q->K);
+          from_row(*q, n0), it, nr, V, dloss + n0, coef + n0, dp + n0 * q->K, at + n0 * q->K, x, H, x2);
     });
+    if (x2 != nullptr) xg = x2;
     prof_end(K_VOC_TEACHER, s);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   }
-  const int n = static_cast<int>(N);
+  const int n = static_cast<int>(N), nr = static_cast<int>(rows);
   for (int64_t b0 = 0; b0 < V; b0 += vblock) {
     const int vb = static_cast<int>(std::min<int64_t>(vblock, V - b0));
-    const int64_t gp = align_up(vb, 8);
+    const int64_t gp = align_up(vb, 8), low = (rows - N) * gp;
     const uint16_t* wb = w;
     int64_t ldw = V, bc0 = b0;
     if (wst != nullptr) {
@@ -737,12 +769,13 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
       bc0 = 0;
     }
     if (q != nullptr) {
-      if (hipError_t e = launch_distill_grad_mfma(x, wb, ldw, bc0, n, H, vb, it, lse, coef, G, gp, s);
+      if (hipError_t e = launch_distill_grad_mfma(x, wb, ldw, bc0, n, H, vb, it, lse, coef, G, gp, low,
+                                                      s);
           e != hipSuccess)
         return e;
       prof_begin(K_VOC_TEACHER, s);
       distill_slots_kernel<<<static_cast<unsigned>(ceil_div(N * q->K, 256)), 256, 0, s>>>(
-          q->K, it, N, b0, vb, coef, dp, at, yk, lse, G, gp);
+          q->K, it, N, b0, vb, coef, dp, at, yk, lse, G, gp, low);
       prof_end(K_VOC_TEACHER, s);
       if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     } else if (hipError_t e = launch_vocab_grad_mfma(x, wb, ldw, bc0, b0, n, H, vb, target, lse,
@@ -750,14 +783,14 @@ hipError_t run_bwd(const uint16_t* x, const uint16_t* w, const int32_t* target, 
                e != hipSuccess) {
       return e;
     }
-    if (hipError_t e = launch_vocab_dx_mfma(G, gp, wb, ldw, bc0, n, H, vb, kspan, b0 == 0, dxa, s);
+    if (hipError_t e = launch_vocab_dx_mfma(G, gp, wb, ldw, bc0, nr, H, vb, kspan, b0 == 0, dxa, s);
         e != hipSuccess)
       return e;
-    if (hipError_t e = launch_vocab_dw_mfma(x, G, gp, n, H, vb, dw, V, b0, s); e != hipSuccess)
+    if (hipError_t e = launch_vocab_dw_mfma(xg, G, gp, nr, H, vb, dw, V, b0, s); e != hipSuccess)
       return e;
   }
-  const int64_t nx = N * H;
-  voc_dx_sum_kernel<<<groups_for(nx / 8), 256, 0, s>>>(dxa, slabs, nx, dx);
+  const int64_t nx = N * H;  // (G's parts are slabs of their own)
+  voc_dx_sum_kernel<<<groups_for(nx / 8), 256, 0, s>>>(dxa, slabs * static_cast<int>(rows / N), nx, dx);
   return hipGetLastError();
 }
 
