@@ -31,11 +31,13 @@
 //
 // Sums, exponentials and log-sum-exps are fp32.  G is the one value held in fewer
 // bits: rounded to bf16 once (off by 2^-8 of itself at most), as the operand of
-// two bf16 matrix products.  Many rounded entries average out in dX and dW (their
-// errors against 64 bits, N = 1000, H = 520, V = 32003: 0.0024 of their norm;
-// rounding the results alone makes 0.0017).  With few rows the roundings of the
-// few large entries, at the teacher's slots, are all there is (up to 0.0034), so
-// distillation then holds G in two bf16 parts (PARTS_ROWS below).
+// two bf16 matrix products.  Entries round independently and average out in dX
+// and dW (their errors against 64 bits, N = 1000, H = 520, V = 32003: 0.0024 of
+// their norm; rounding the results alone makes 0.0017), but for the large ones, at
+// the teacher's slots, where these are alike: equal dl and probabilities near one
+// all round the same way (N = 502, V = 121106, two slots: 0.0029).  With few rows
+// such entries are all there is (up to 0.0034), so distillation then holds G in
+// two bf16 parts (PARTS_ROWS below).
 #include "common.h"
 
 #include <algorithm>
