@@ -243,13 +243,14 @@ def _mix(x, k):
 
 def _random(group, first):
     """Two times 16 bits for each element of a group's tensors (numbered from
-    `first`): of the element's place in its tensor, the tensor's number and the
-    seed."""
+    `first`): of the element's place in its tensor, the tensor's number, the step
+    and the seed."""
     dev = group["g"].device
     at = torch.tensor(group["at"], device=dev)
     n = at[1:] - at[:-1]
     j = torch.arange(first, first + n.numel(), device=dev)
-    key = _mix(_mix((SEED + j * 0x9E3779B9) & 0xFFFFFFFF, 0x6A09E667), 0xBB67AE85)
+    key = (SEED + STEP * 0x85A308D3 + j * 0x9E3779B9) & 0xFFFFFFFF
+    key = _mix(_mix(key, 0x6A09E667), 0xBB67AE85)
     x = torch.arange(group["at"][-1], device=dev) - at[:-1].repeat_interleave(n)
     x = (x * 0x9E3779B9 + key.repeat_interleave(n)) & 0xFFFFFFFF
     return _mix(x, 0x6A09E667)
