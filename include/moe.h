@@ -522,6 +522,143 @@ int moe_vocab_distill_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_
                           moe_bf16* dw_voc, void* workspace, size_t workspace_bytes,
                           void* stream);
 
+/* --------------------------------------------------------------- embedding
+ * Embedding of tokens (Sec. 3.2 keeps it with the dense weights), over this
+ * rank's rows [begin, begin + rows) of the vocabulary:
+ *   y[t] = bf16(scale w[ids[t] - begin]); 0 where ids[t] is outside them (another
+ *          rank's, or -1 for padding), so that the ranks' outputs add up
+ *   dw[v] = bf16(scale sum of dy[t] over the tokens with ids[t] = begin + v)
+ * The sums are fp32 in an order that only the ids set (runs of ascending t, joined
+ * in order): equal bits run to run.  Every row of dw is written, those without
+ * tokens as zeros.  A NaN in dy stays in its row.
+ *
+ * ids [N] int32; w, dw [rows][H] bf16; y, dy [N][H] bf16.  Limits: 0 <= N < 2^26,
+ * 1 <= rows < 2^28, begin + rows <= 2^31, N * H < 2^38, scale finite.  Workspace
+ * (none for N = 0): the sorted tokens and fp32 sums of runs cut at every 8 to 64
+ * sorted tokens, at most N H bytes and 24 N, and 1 MiB.
+ */
+int moe_embedding_fwd(const int32_t* ids, const moe_bf16* w, int64_t N, int H, int64_t begin,
+                      int64_t rows, float scale, moe_bf16* y, void* stream);
+int moe_embedding_bwd_workspace_bytes(int64_t N, int H, int64_t rows, size_t* bytes);
+int moe_embedding_bwd(const int32_t* ids, const moe_bf16* dy, int64_t N, int H, int64_t begin,
+                      int64_t rows, float scale, moe_bf16* dw, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/* -------------------------------------------------------------- layer norm
+ * Layer norm of each row, with the residual sum that goes before it:
+ *   h = bf16(x + residual) (with residual = NULL: x itself, and h is not written)
+ *   mean = sum_j h_j / d, rstd = 1 / sqrt(sum_j (h_j - mean)^2 / d + eps)
+ *   y_j = bf16((h_j - mean) rstd gamma_j + beta_j)         (beta = NULL: 0)
+ * and, given dy = dL/dy and dh = dL/dh of what else reads h (NULL: nothing), with
+ * xh_j = (h_j - mean) rstd and g_j = dy_j gamma_j:
+ *   dx_j = bf16(dh_j + rstd (g_j - sum g / d - xh_j sum(g xh) / d))
+ *          (the gradient of x and of residual alike)
+ *   dgamma_j = sum over rows of dy_j xh_j, dbeta_j = sum over rows of dy_j
+ * Statistics and sums are fp32 in a fixed order.  x, residual, h, y, dy, dh, dx
+ * [T][d] bf16; gamma, beta, dgamma, dbeta [d] fp32; mean, rstd [T] fp32 (NULL in
+ * the forward: not wanted; the backward takes them back).  dbeta may be NULL.
+ * T = 0 is valid: dgamma and dbeta become zeros.  A NaN or infinity stays in its
+ * row, but reaches dgamma and dbeta.  Limits: 0 <= T < 2^31, eps > 0.
+ */
+int moe_layer_norm_fwd(const moe_bf16* x, const moe_bf16* residual, const float* gamma,
+                       const float* beta, int64_t T, int d, float eps, moe_bf16* h, moe_bf16* y,
+                       float* mean, float* rstd, void* stream);
+int moe_layer_norm_bwd_workspace_bytes(int64_t T, int d, size_t* bytes);
+int moe_layer_norm_bwd(const moe_bf16* dy, const moe_bf16* h, const float* gamma,
+                       const float* mean, const float* rstd, const moe_bf16* dh, int64_t T, int d,
+                       moe_bf16* dx, float* dgamma, float* dbeta, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* --------------------------------------------------------- weight updates
+ * AdamW over a list of tensors in one call (Sec. 3.5 keeps its fp32 states on the
+ * host; with 288 GB a device holds them, and in 8 bits a quarter of them).
+ *
+ * moe_param names one tensor of n elements (n = 0: left out): weights w, fp32 or
+ * bf16 (w_type); with fp32 weights optionally a bf16 copy of them, written with
+ * every step; gradient g, fp32 or bf16; states m and v, fp32 [n], or 8-bit codes
+ * [n] with a scale byte for each 128 elements (m_scale, v_scale [ceil(n / 128)],
+ * of any alignment).  All zeros are the states before the first step, in either
+ * form.  The list itself is host memory, read before the call returns; what it
+ * names is device memory, and what a call writes overlaps nothing else in it.
+ */
+enum { MOE_F32 = 0, MOE_BF16 = 1 };
+typedef struct moe_param {
+  void* w;
+  moe_bf16* w_copy;
+  const void* g;
+  void* m;
+  void* v;
+  uint8_t* m_scale;
+  uint8_t* v_scale;
+  int64_t n;
+  int32_t w_type;
+  int32_t g_type;
+} moe_param;
+
+/* sumsq[0] = sum over all gradients' elements of g^2 (reads g, g_type and n only):
+ * fp32 squares and short sums, joined in 64 bits, in a fixed order; a value above
+ * 1.8e19 gives inf.  0 for an empty list.  Ranks that hold parts of a model add
+ * theirs up before the step.
+ */
+int moe_grad_sumsq_workspace_bytes(const moe_param* params, int count, size_t* bytes);
+int moe_grad_sumsq(const moe_param* params, int count, float* sumsq, void* workspace,
+                   size_t workspace_bytes, void* stream);
+
+/* One step, for every element, in fp32:
+ *   g' = c g,  c = max_norm / max(sqrt(grad_sumsq[0]), max_norm)  (1 without it)
+ *   m' = beta1 m + (1 - beta1) g',  v' = beta2 v + (1 - beta2) g'^2
+ *   w' = (1 - lr weight_decay) w
+ *        - lr / (1 - beta1^t) m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
+ * t = step >= 1.  lr_device, step_device (device scalars, NULL: not used) take the
+ * place of lr and step, so that a captured step replays with new ones (a step
+ * below 1 counts as 1).  Where grad_sumsq is given and its value is negative, not
+ * finite or NaN, nothing is updated: a step whose gradients overflowed is left out.
+ *
+ * 8-bit states (bits = 8).  Each block of 128 elements has a power of two
+ * u = 2^(s - 127), s its scale byte: 14 (m) or 30 (v) below the exponent of the
+ * block's largest |m'| or v', 1 at least; 255 where that is not finite (the block
+ * then stands for NaN).  A code c = 8 k + j, j < 8, stands for
+ * u (2^k (1 + j / 8) - 1); m has a sign in bit 7 and 7 bits of code, v 8 bits of
+ * code.  The update uses m' and v' unrounded; to be held, |x| + u is rounded up or
+ * down to a code with the probability that makes the mean right, and v' > 0 has
+ * code 1 at least.  m' and v' are formed without fused operations, and the 16 random
+ * bits of an element are fixed (all in 32-bit integers that wrap):
+ *   mix(x, q): x ^= x >> 16; x *= q; x ^= x >> 15
+ *   key = mix(mix(seed + 0x85A308D3 t + 0x9E3779B9 j, 0x6A09E667), 0xBB67AE85),
+ *         j the tensor's place in the list
+ *   r = mix(0x9E3779B9 i + key, 0x6A09E667), i the element's place in its tensor;
+ *   the low half of r is m's, the high half v's;
+ *   code = (bits(|x| + u) + 16 r16 + 8) >> 20, less 8 s
+ * so codes are a function of the inputs, bit for bit.  bf16 weights (with either
+ * form of state) are rounded to bf16 the same way, by the high half of
+ * r * 0xBB67AE85 (not to the nearest, which would lose steps under half of a
+ * weight's last bit); the copy of fp32 weights is rounded to the nearest.
+ *
+ * Limits: bits 8 or 32; 0 <= beta < 1, eps >= 1e-30, max_norm > 0 (infinity: no
+ * clipping, but steps are left out as above), n < 2^40, t < 2^31.
+ */
+typedef struct moe_adamw_options {
+  double lr;
+  double beta1;
+  double beta2;
+  double eps;
+  double weight_decay;
+  int64_t step;
+  const float* lr_device;
+  const int32_t* step_device;
+  const float* grad_sumsq;
+  double max_norm;
+  uint32_t seed;
+} moe_adamw_options;
+int moe_adamw_step(const moe_param* params, int count, int bits, const moe_adamw_options* options,
+                   void* stream);
+
+/* The values of 8-bit states: m[i], v[i] [params[i].n] fp32 (host lists of device
+ * pointers), for checkpoints and for going on with 32-bit states.
+ */
+int moe_adamw_states(const moe_param* params, int count, float* const* m, float* const* v,
+                     void* stream);
+
 /* ------------------------------------------ least-loaded expert parallelism
  * Sec. 3.3 (recap of LLEP): the load of each rank is taken at every call
  * of the layer; a rank above its share hands some of its token-expert

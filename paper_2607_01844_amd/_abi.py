@@ -35,6 +35,9 @@ C_SYMBOLS = (
     "moe_ffn_fwd_mxfp4_workspace_bytes", "moe_ffn_fwd_mxfp4",
     "moe_vocab_loss_workspace_bytes", "moe_vocab_loss_fwd", "moe_vocab_loss_bwd",
     "moe_vocab_distill_workspace_bytes", "moe_vocab_distill_fwd", "moe_vocab_distill_bwd",
+    "moe_embedding_fwd", "moe_embedding_bwd_workspace_bytes", "moe_embedding_bwd",
+    "moe_layer_norm_fwd", "moe_layer_norm_bwd_workspace_bytes", "moe_layer_norm_bwd",
+    "moe_grad_sumsq_workspace_bytes", "moe_grad_sumsq", "moe_adamw_step", "moe_adamw_states",
     "moe_llep_plan", "moe_llep_dispatch",
     "moe_profile_enable", "moe_profile_reset", "moe_profile_num_kernels",
     "moe_profile_kernel_name", "moe_profile_query",
@@ -43,6 +46,27 @@ C_SYMBOLS = (
 
 class MoEError(RuntimeError):
     pass
+
+
+MOE_F32 = 0
+MOE_BF16 = 1
+
+
+class Param(ctypes.Structure):
+    """moe_param"""
+    _fields_ = [("w", ctypes.c_void_p), ("w_copy", ctypes.c_void_p), ("g", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n", ctypes.c_int64), ("w_type", ctypes.c_int32),
+                ("g_type", ctypes.c_int32)]
+
+
+class AdamWOptions(ctypes.Structure):
+    """moe_adamw_options"""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("step", ctypes.c_int64), ("lr_device", ctypes.c_void_p),
+                ("step_device", ctypes.c_void_p), ("grad_sumsq", ctypes.c_void_p),
+                ("max_norm", ctypes.c_double), ("seed", ctypes.c_uint32)]
 
 
 def load(path: str = None):
@@ -98,6 +122,16 @@ def load(path: str = None):
         "moe_vocab_distill_fwd": ([P, P, P, P, P, F, I64, I, I64, I64, I, P, P, P, P, SZ, P], I),
         "moe_vocab_distill_bwd": ([P, P, P, P, P, F, P, P, P, I64, I, I64, I64, I, P, P, P, SZ, P],
                                   I),
+        "moe_embedding_fwd": ([P, P, I64, I, I64, I64, F, P, P], I),
+        "moe_embedding_bwd_workspace_bytes": ([I64, I, I64, PSZ], I),
+        "moe_embedding_bwd": ([P, P, I64, I, I64, I64, F, P, P, SZ, P], I),
+        "moe_layer_norm_fwd": ([P, P, P, P, I64, I, F, P, P, P, P, P], I),
+        "moe_layer_norm_bwd_workspace_bytes": ([I64, I, PSZ], I),
+        "moe_layer_norm_bwd": ([P, P, P, P, P, P, I64, I, P, P, P, P, SZ, P], I),
+        "moe_grad_sumsq_workspace_bytes": ([P, I, PSZ], I),
+        "moe_grad_sumsq": ([P, I, P, P, SZ, P], I),
+        "moe_adamw_step": ([P, I, I, P, P], I),
+        "moe_adamw_states": ([P, I, P, P, P], I),
         "moe_llep_plan": ([P, I, I, I, I, P, P, P, P, P], I),
         "moe_llep_dispatch": ([P, P, P, P, P, P, I, I, I64, I, I, I, I64, P, P, P, P, P], I),
         "moe_profile_enable": ([I], I),

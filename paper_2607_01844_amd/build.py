@@ -23,7 +23,7 @@ LIB = os.path.join(PKG, "libmoe.so")
 DEVICE_TEXT = os.path.join(PKG, "libmoe.device_text.json")
 SOURCES = ["api.hip", "route.hip", "route_bwd.hip", "permute.hip", "combine.hip", "gemm.hip",
            "gemm_small.hip", "chunked.hip", "vocab.hip", "llep.hip", "balance.hip",
-           "mxfp4.hip"]
+           "mxfp4.hip", "embed.hip", "norm.hip", "optim.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

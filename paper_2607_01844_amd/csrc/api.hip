@@ -2,6 +2,7 @@
 // any HIP call), workspace queries, status strings and the optional
 // per-kernel event profiler.  Kernels live in route/permute/combine/gemm.hip.
 #include <atomic>
+#include <cmath>
 #include <cstdio>
 #include <mutex>
 #include <string>
@@ -91,7 +92,9 @@ const char* const kNames[moe::K_NUM] = {
     "route_dw",     "route_dx",        "vocab_lse",          "vocab_grad",    "llep_plan",     "llep_window",
     "route_split",  "vocab_logits",    "vocab_dx",           "vocab_dw",
     "balance_part", "balance_sum",     "balance_bwd",        "vocab_teacher",
-    "mx_quantize",  "mx_gate_up",      "mx_down"};
+    "mx_quantize",  "mx_gate_up",      "mx_down",            "embed",
+    "embed_sort",   "embed_sum",       "norm_fwd",           "norm_bwd",
+    "norm_sum",     "grad_sumsq",      "adamw",              "adamw_states"};
 
 }  // namespace
 
@@ -851,6 +854,192 @@ MOE_API int moe_llep_dispatch(const moe_bf16* x, const int32_t* topk_idx,
   return hip_status(moe::launch_llep_dispatch(x, topk_idx, offsets_all, dst_all, win_lo + o,
                                               win_hi + o, T, d, E, k, cap, offsets_r, row_src_r,
                                               dst_r, x_perm_r, static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+// --------------------------------------------------------------- embedding
+static int check_embed(const char* fn, int64_t N, int H, int64_t begin, int64_t rows, float scale) {
+  CHECK(N >= 0 && N < (int64_t{1} << 26), "N out of [0, 2^26)");
+  if (int r = check_dim(fn, H, "H")) return r;
+  CHECK(N * H < (int64_t{1} << 38), "N*H >= 2^38");
+  CHECK(rows >= 1 && rows < (int64_t{1} << 28), "rows out of [1, 2^28)");
+  CHECK(begin >= 0 && begin <= (int64_t{1} << 31) - rows, "row range outside [0, 2^31)");
+  CHECK(std::isfinite(scale), "scale is not finite");
+  return MOE_OK;
+}
+
+MOE_API int moe_embedding_fwd(const int32_t* ids, const moe_bf16* w, int64_t N, int H,
+                              int64_t begin, int64_t rows, float scale, moe_bf16* y, void* stream) {
+  const char* fn = "moe_embedding_fwd";
+  if (int r = check_embed(fn, N, H, begin, rows, scale)) return r;
+  if (N > 0) {
+    REQ(ids); REQ(w); REQ(y);
+  }
+  return hip_status(moe::launch_embed_fwd(ids, w, N, H, begin, rows, scale, y,
+                                          static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+MOE_API int moe_embedding_bwd_workspace_bytes(int64_t N, int H, int64_t rows, size_t* bytes) {
+  const char* fn = "moe_embedding_bwd_workspace_bytes";
+  CHECK(bytes != nullptr, "bytes is NULL");
+  if (int r = check_embed(fn, N, H, 0, rows, 1.0f)) return r;
+  *bytes = moe::embed_bwd_ws_bytes(N, H, rows);
+  return MOE_OK;
+}
+
+MOE_API int moe_embedding_bwd(const int32_t* ids, const moe_bf16* dy, int64_t N, int H,
+                              int64_t begin, int64_t rows, float scale, moe_bf16* dw,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  const char* fn = "moe_embedding_bwd";
+  if (int r = check_embed(fn, N, H, begin, rows, scale)) return r;
+  REQ(dw);
+  if (N > 0) {
+    REQ(ids); REQ(dy);
+    if (workspace == nullptr || workspace_bytes < moe::embed_bwd_ws_bytes(N, H, rows))
+      return fail(MOE_ERR_WORKSPACE, fn, "workspace smaller than moe_embedding_bwd_workspace_bytes()");
+    OPT(workspace);
+  }
+  return hip_status(moe::launch_embed_bwd(ids, dy, N, H, begin, rows, scale, dw, workspace,
+                                          static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+// -------------------------------------------------------------- layer norm
+static int check_norm(const char* fn, int64_t T, int d) {
+  CHECK(T >= 0 && T < (int64_t{1} << 31), "T out of [0, 2^31)");
+  return check_dim(fn, d, "d");
+}
+
+MOE_API int moe_layer_norm_fwd(const moe_bf16* x, const moe_bf16* residual, const float* gamma,
+                               const float* beta, int64_t T, int d, float eps, moe_bf16* h,
+                               moe_bf16* y, float* mean, float* rstd, void* stream) {
+  const char* fn = "moe_layer_norm_fwd";
+  if (int r = check_norm(fn, T, d)) return r;
+  CHECK(std::isfinite(eps) && eps > 0.0f, "eps must be positive and finite");
+  if (T > 0) {
+    REQ(x); REQ(gamma); REQ(y);
+    OPT(residual); OPT(beta); OPT(mean); OPT(rstd);
+    if (residual != nullptr) REQ(h);
+  }
+  return hip_status(moe::launch_norm_fwd(x, residual, gamma, beta, T, d, eps, h, y, mean, rstd,
+                                         static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+MOE_API int moe_layer_norm_bwd_workspace_bytes(int64_t T, int d, size_t* bytes) {
+  const char* fn = "moe_layer_norm_bwd_workspace_bytes";
+  CHECK(bytes != nullptr, "bytes is NULL");
+  if (int r = check_norm(fn, T, d)) return r;
+  *bytes = moe::norm_bwd_ws_bytes(T, d);
+  return MOE_OK;
+}
+
+MOE_API int moe_layer_norm_bwd(const moe_bf16* dy, const moe_bf16* h, const float* gamma,
+                               const float* mean, const float* rstd, const moe_bf16* dh, int64_t T,
+                               int d, moe_bf16* dx, float* dgamma, float* dbeta, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  const char* fn = "moe_layer_norm_bwd";
+  if (int r = check_norm(fn, T, d)) return r;
+  REQ(dgamma);
+  OPT(dbeta);
+  if (T > 0) {
+    REQ(dy); REQ(h); REQ(gamma); REQ(mean); REQ(rstd); REQ(dx);
+    OPT(dh);
+    if (workspace == nullptr || workspace_bytes < moe::norm_bwd_ws_bytes(T, d))
+      return fail(MOE_ERR_WORKSPACE, fn, "workspace smaller than moe_layer_norm_bwd_workspace_bytes()");
+    OPT(workspace);
+  }
+  return hip_status(moe::launch_norm_bwd(dy, h, gamma, mean, rstd, dh, T, d, dx, dgamma, dbeta,
+                                         workspace, static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+// ------------------------------------------------------- lists of tensors
+static int check_grads(const char* fn, const moe_param* params, int count) {
+  CHECK(count >= 0, "count < 0");
+  CHECK(count == 0 || params != nullptr, "params is NULL");
+  for (int i = 0; i < count; ++i) {
+    const moe_param& p = params[i];
+    CHECK(p.n >= 0 && p.n < (int64_t{1} << 40), "n out of [0, 2^40)");
+    CHECK(p.g_type == MOE_F32 || p.g_type == MOE_BF16, "g_type must be MOE_F32 or MOE_BF16");
+    if (p.n > 0) REQ(p.g);
+  }
+  return MOE_OK;
+}
+static int check_states(const char* fn, const moe_param* params, int count, int bits) {
+  for (int i = 0; i < count; ++i) {
+    const moe_param& p = params[i];
+    CHECK(p.n >= 0 && p.n < (int64_t{1} << 40), "n out of [0, 2^40)");
+    if (p.n == 0) continue;
+    REQ(p.m); REQ(p.v);
+    CHECK(bits == 32 || (p.m_scale != nullptr && p.v_scale != nullptr),
+          "8-bit states need m_scale and v_scale");
+  }
+  return MOE_OK;
+}
+
+MOE_API int moe_grad_sumsq_workspace_bytes(const moe_param* params, int count, size_t* bytes) {
+  const char* fn = "moe_grad_sumsq_workspace_bytes";
+  CHECK(bytes != nullptr, "bytes is NULL");
+  if (int r = check_grads(fn, params, count)) return r;
+  *bytes = moe::grad_sumsq_ws_bytes(params, count);
+  return MOE_OK;
+}
+
+MOE_API int moe_grad_sumsq(const moe_param* params, int count, float* sumsq, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  const char* fn = "moe_grad_sumsq";
+  if (int r = check_grads(fn, params, count)) return r;
+  REQ(sumsq);
+  if (workspace == nullptr || workspace_bytes < moe::grad_sumsq_ws_bytes(params, count))
+    return fail(MOE_ERR_WORKSPACE, fn, "workspace smaller than moe_grad_sumsq_workspace_bytes()");
+  OPT(workspace);
+  return hip_status(moe::launch_grad_sumsq(params, count, sumsq, workspace,
+                                           static_cast<hipStream_t>(stream)),
+                    fn);
+}
+
+MOE_API int moe_adamw_step(const moe_param* params, int count, int bits,
+                           const moe_adamw_options* options, void* stream) {
+  const char* fn = "moe_adamw_step";
+  if (int r = check_grads(fn, params, count)) return r;
+  CHECK(bits == 8 || bits == 32, "bits must be 8 or 32");
+  CHECK(options != nullptr, "options is NULL");
+  const moe_adamw_options& o = *options;
+  CHECK(o.lr_device != nullptr || std::isfinite(o.lr), "lr is not finite");
+  CHECK(o.beta1 >= 0.0 && o.beta1 < 1.0, "beta1 out of [0, 1)");
+  CHECK(o.beta2 >= 0.0 && o.beta2 < 1.0, "beta2 out of [0, 1)");
+  CHECK(std::isfinite(o.eps) && o.eps >= 1e-30, "eps must be finite and 1e-30 or more");
+  CHECK(std::isfinite(o.weight_decay), "weight_decay is not finite");
+  CHECK(o.step_device != nullptr || (o.step >= 1 && o.step < (int64_t{1} << 31)),
+        "step out of [1, 2^31)");
+  CHECK(o.grad_sumsq == nullptr || o.max_norm > 0.0, "max_norm must be positive");
+  OPT(o.lr_device); OPT(o.step_device); OPT(o.grad_sumsq);
+  if (int r = check_states(fn, params, count, bits)) return r;
+  for (int i = 0; i < count; ++i) {
+    const moe_param& p = params[i];
+    CHECK(p.w_type == MOE_F32 || p.w_type == MOE_BF16, "w_type must be MOE_F32 or MOE_BF16");
+    if (p.n > 0) REQ(p.w);
+    OPT(p.w_copy);
+    CHECK(p.w_copy == nullptr || p.w_type == MOE_F32, "w_copy needs fp32 weights");
+  }
+  return hip_status(moe::launch_adamw(params, count, bits, o, static_cast<hipStream_t>(stream)), fn);
+}
+
+MOE_API int moe_adamw_states(const moe_param* params, int count, float* const* m, float* const* v,
+                             void* stream) {
+  const char* fn = "moe_adamw_states";
+  CHECK(count >= 0, "count < 0");
+  CHECK(count == 0 || (params != nullptr && m != nullptr && v != nullptr),
+        "params, m or v is NULL");
+  if (int r = check_states(fn, params, count, 8)) return r;
+  for (int i = 0; i < count; ++i)
+    if (params[i].n > 0) {
+      REQ(m[i]); REQ(v[i]);
+    }
+  return hip_status(moe::launch_adamw_states(params, count, m, v,
+                                             static_cast<hipStream_t>(stream)),
                     fn);
 }
 

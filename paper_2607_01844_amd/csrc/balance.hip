@@ -19,35 +19,6 @@
 namespace moe {
 namespace {
 
-// Over the lanes l, l ^ 1, .., of aligned groups of N lanes, in every one of them:
-// within 16 lanes by lane permutations of the vector unit (mirrors serve as
-// exchanges, the smaller groups being equal already), then by row and half swaps.
-template <int CTRL>
-__device__ __forceinline__ float moved(float v) {
-  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xf, 0xf, true));
-}
-template <int N, typename F>
-__device__ __forceinline__ float over_lanes(float v, F&& f) {
-  if constexpr (N > 1) v = f(v, moved<0xb1>(v));    // quad_perm 1 0 3 2
-  if constexpr (N > 2) v = f(v, moved<0x4e>(v));    // quad_perm 2 3 0 1
-  if constexpr (N > 4) v = f(v, moved<0x141>(v));   // half a row mirrored
-  if constexpr (N > 8) v = f(v, moved<0x140>(v));   // a row mirrored
-  if constexpr (N > 16) {
-    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = f(__uint_as_float(t[0]), __uint_as_float(t[1]));
-  }
-  if constexpr (N > 32) {
-    const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = f(__uint_as_float(t[0]), __uint_as_float(t[1]));
-  }
-  return v;
-}
-struct Sum {
-  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
-};
-struct Max {
-  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
-};
 // The sum over the lanes that differ in multiples of N only (the same place in
 // every group of N): turns of 16 lanes, then the swaps.
 template <int N, typename T>

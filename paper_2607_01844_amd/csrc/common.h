@@ -44,6 +44,35 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// Over the lanes l, l ^ 1, .., of aligned groups of N lanes, in every one of them:
+// within 16 lanes by lane permutations of the vector unit (mirrors serve as
+// exchanges, the smaller groups being equal already), then by row and half swaps.
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+template <int N, typename F>
+__device__ __forceinline__ float over_lanes(float v, F&& f) {
+  if constexpr (N > 1) v = f(v, moved<0xb1>(v));    // quad_perm 1 0 3 2
+  if constexpr (N > 2) v = f(v, moved<0x4e>(v));    // quad_perm 2 3 0 1
+  if constexpr (N > 4) v = f(v, moved<0x141>(v));   // half a row mirrored
+  if constexpr (N > 8) v = f(v, moved<0x140>(v));   // a row mirrored
+  if constexpr (N > 16) {
+    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(t[0]), __uint_as_float(t[1]));
+  }
+  if constexpr (N > 32) {
+    const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(t[0]), __uint_as_float(t[1]));
+  }
+  return v;
+}
+struct Sum {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+struct Max {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
 // Compile-time loop: f(std::integral_constant<int, 0..N-1>) (keeps register
 // arrays indexed by constants, so they never fall back to scratch memory).
 template <typename F, int... Is>
@@ -98,6 +127,15 @@ enum KernelId {
   K_MX_QUANT,
   K_MX_GATE_UP,
   K_MX_DOWN,
+  K_EMBED,
+  K_EMBED_SORT,
+  K_EMBED_SUM,
+  K_NORM_FWD,
+  K_NORM_BWD,
+  K_NORM_SUM,
+  K_GRAD_SUMSQ,
+  K_ADAMW,
+  K_ADAMW_STATES,
   K_NUM
 };
 
@@ -270,6 +308,30 @@ hipError_t launch_mx_layer(const uint16_t* x, const int32_t* idx, const float* g
                            int d, int E, int k, int e_begin, int E_loc, int f,
                            const uint8_t* const wq[3], const uint8_t* const wsc[3], uint16_t* y,
                            void* ws, hipStream_t s);
+// Embedding of tokens whose rows lie in [begin, begin + rows), and its gradient.
+hipError_t launch_embed_fwd(const int32_t* ids, const uint16_t* w, int64_t N, int H, int64_t begin,
+                            int64_t rows, float scale, uint16_t* y, hipStream_t s);
+size_t embed_bwd_ws_bytes(int64_t N, int H, int64_t rows);
+hipError_t launch_embed_bwd(const int32_t* ids, const uint16_t* dy, int64_t N, int H, int64_t begin,
+                            int64_t rows, float scale, uint16_t* dw, void* ws, hipStream_t s);
+// Layer norm of x (+ res, with the sum in h), and its gradient.
+hipError_t launch_norm_fwd(const uint16_t* x, const uint16_t* res, const float* gamma,
+                           const float* beta, int64_t T, int d, float eps, uint16_t* h,
+                           uint16_t* y, float* mean, float* rstd, hipStream_t s);
+size_t norm_bwd_ws_bytes(int64_t T, int d);
+hipError_t launch_norm_bwd(const uint16_t* dy, const uint16_t* h, const float* gamma,
+                           const float* mean, const float* rstd, const uint16_t* dh, int64_t T,
+                           int d, uint16_t* dx, float* dgamma, float* dbeta, void* ws,
+                           hipStream_t s);
+// Lists of tensors: the gradients' sum of squares, an AdamW step, and 8-bit
+// states as values.
+size_t grad_sumsq_ws_bytes(const moe_param* params, int count);
+hipError_t launch_grad_sumsq(const moe_param* params, int count, float* sumsq, void* ws,
+                             hipStream_t s);
+hipError_t launch_adamw(const moe_param* params, int count, int bits, const moe_adamw_options& opt,
+                        hipStream_t s);
+hipError_t launch_adamw_states(const moe_param* params, int count, float* const* m, float* const* v,
+                               hipStream_t s);
 hipError_t launch_ffn_fwd(const uint16_t* x_perm, const int32_t* offsets, int E_loc, int64_t cap,
                           int d, int f, const uint16_t* wg, const uint16_t* wu,
                           const uint16_t* wd, uint16_t* hg, uint16_t* hu, uint16_t* y,

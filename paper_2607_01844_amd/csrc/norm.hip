@@ -1,0 +1,530 @@
+// Layer norm of rows of bf16, forward (with the residual sum) and backward (gfx950).
+//   h = bf16(x + residual), mu = mean h, r = 1 / sqrt(mean (h - mu)^2 + eps),
+//   y = (h - mu) r gamma + beta;
+//   with xh = (h - mu) r and g = dy gamma:
+//   dx = dh + r (g - mean g - xh mean(g xh)), dgamma = sum_t dy xh, dbeta = sum_t dy.
+// A row is held in registers by W waves, so each operand crosses HBM once; the
+// mean is subtracted before the squares are summed (a row far from zero keeps its
+// variance).  Sums, statistics and the weights' gradients are fp32; every
+// bf16 result is rounded once.  Bound by the HBM stream.
+#include <algorithm>
+
+#include "common.h"
+
+namespace moe {
+namespace {
+
+__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
+  f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x);
+  f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+  f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z);
+  f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                    pack_bf16x2(f[6], f[7]));
+}
+__device__ __forceinline__ uint4 add8(const uint4& a, const uint4& b) {
+  float f[8], g[8];
+  unpack8(a, f);
+  unpack8(b, g);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) f[q] += g[q];
+  return pack8(f);
+}
+__device__ __forceinline__ void load8f(const float* __restrict__ p, float* f) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+  f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+
+// Over the W waves of a row: the sums of n values, in every lane.  `red` is this
+// exchange's own place; with two exchanges a round, one barrier each is enough.
+template <int W, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float* red, int w, int lane) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = over_lanes<64>(v[i], Sum());
+  if constexpr (W > 1) {
+    if (lane == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) red[i * W + w] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = red[i * W];
+#pragma unroll
+      for (int u = 1; u < W; ++u) v[i] += red[i * W + u];
+    }
+  }
+}
+
+// Waves of a row W, chunks of 8 columns a lane C, rows at once R.  Chunk c of
+// lane l of wave w: (c W + w) 64 + l.
+template <int W, int C, int R, bool RES>
+__global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_fwd_kernel(
+    const uint16_t* __restrict__ x, const uint16_t* __restrict__ res,
+    const float* __restrict__ gamma, const float* __restrict__ beta, int64_t T, int d, float eps,
+    uint16_t* __restrict__ h, uint16_t* __restrict__ y, float* __restrict__ mean,
+    float* __restrict__ rstd) {
+  constexpr int G = W < 4 ? 4 / W : 1;  // rows' teams of a workgroup
+  __shared__ float red[2][R * W];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int w = wave % W, team = wave / W;
+  const int nch = d >> 3;
+  const float fd = static_cast<float>(d);
+  float ga[C][8], be[C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int at = (c * W + w) * 64 + lane;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) be[c][q] = 0.0f;
+    if (at < nch) {
+      load8f(gamma + 8 * at, ga[c]);
+      if (beta) load8f(beta + 8 * at, be[c]);
+    }
+  }
+  const int64_t step = static_cast<int64_t>(gridDim.x) * G * R;
+  for (int64_t t0 = (static_cast<int64_t>(blockIdx.x) * G + team) * R; t0 < T; t0 += step) {
+    uint4 v[R][C], e[R][C];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int at = (c * W + w) * 64 + lane;
+        v[r][c] = make_uint4(0, 0, 0, 0);
+        if (at < nch && t0 + r < T) {
+          v[r][c] = reinterpret_cast<const uint4*>(x + (t0 + r) * d)[at];
+          if constexpr (RES) e[r][c] = reinterpret_cast<const uint4*>(res + (t0 + r) * d)[at];
+        }
+      }
+    if constexpr (RES) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int at = (c * W + w) * 64 + lane;
+          if (at < nch && t0 + r < T) {
+            v[r][c] = add8(v[r][c], e[r][c]);
+            reinterpret_cast<uint4*>(h + (t0 + r) * d)[at] = v[r][c];
+          }
+        }
+    }
+    float mu[R], sq[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mu[r] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float f[8];
+        unpack8(v[r][c], f);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) mu[r] += f[q];
+      }
+    }
+    row_sums<W>(mu, red[0], w, lane);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mu[r] /= fd;
+      sq[r] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float f[8];
+        unpack8(v[r][c], f);
+        if ((c * W + w) * 64 + lane < nch)
+#pragma unroll
+          for (int q = 0; q < 8; ++q) sq[r] += (f[q] - mu[r]) * (f[q] - mu[r]);
+      }
+    }
+    row_sums<W>(sq, red[1], w, lane);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float rs = 1.0f / sqrtf(sq[r] / fd + eps);
+      if (t0 + r < T) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int at = (c * W + w) * 64 + lane;
+          float f[8];
+          unpack8(v[r][c], f);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) f[q] = (f[q] - mu[r]) * rs * ga[c][q] + be[c][q];
+          if (at < nch) reinterpret_cast<uint4*>(y + (t0 + r) * d)[at] = pack8(f);
+        }
+        if (w == 0 && lane == 0) {
+          if (mean) mean[t0 + r] = mu[r];
+          if (rstd) rstd[t0 + r] = rs;
+        }
+      }
+    }
+  }
+}
+
+// part [workgroups][2][d]: the workgroup's sums of dy xh and of dy.
+template <int W, int C, int R, bool DH>
+__global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_bwd_kernel(
+    const uint16_t* __restrict__ dy, const uint16_t* __restrict__ h,
+    const float* __restrict__ gamma, const float* __restrict__ mean,
+    const float* __restrict__ rstd, const uint16_t* __restrict__ dh, int64_t T, int d,
+    uint16_t* __restrict__ dx, float* __restrict__ part) {
+  constexpr int G = W < 4 ? 4 / W : 1;
+  __shared__ float red[2][2 * R * W];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int w = wave % W, team = wave / W;
+  const int nch = d >> 3;
+  const float fd = static_cast<float>(d);
+  float ga[C][8], dg[C][8], db[C][8];
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int at = (c * W + w) * 64 + lane;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) ga[c][q] = dg[c][q] = db[c][q] = 0.0f;
+    if (at < nch) load8f(gamma + 8 * at, ga[c]);
+  }
+  const int64_t step = static_cast<int64_t>(gridDim.x) * G * R;
+  int turn = 0;
+  for (int64_t t0 = (static_cast<int64_t>(blockIdx.x) * G + team) * R; t0 < T; t0 += step) {
+    uint4 a[R][C], b[R][C], e[R][C];
+    float mu[R], rs[R], s[2 * R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool in = t0 + r < T;
+      mu[r] = in ? mean[t0 + r] : 0.0f;
+      rs[r] = in ? rstd[t0 + r] : 0.0f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int at = (c * W + w) * 64 + lane;
+        a[r][c] = b[r][c] = make_uint4(0, 0, 0, 0);
+        if (at < nch && in) {
+          a[r][c] = reinterpret_cast<const uint4*>(dy + (t0 + r) * d)[at];
+          b[r][c] = reinterpret_cast<const uint4*>(h + (t0 + r) * d)[at];
+          if constexpr (DH) e[r][c] = reinterpret_cast<const uint4*>(dh + (t0 + r) * d)[at];
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      s[2 * r] = s[2 * r + 1] = 0.0f;
+      if (t0 + r < T) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          if ((c * W + w) * 64 + lane < nch) {
+            float f[8], g[8];
+            unpack8(a[r][c], g);
+            unpack8(b[r][c], f);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const float xh = (f[q] - mu[r]) * rs[r];
+              dg[c][q] += g[q] * xh;
+              db[c][q] += g[q];
+              s[2 * r] += g[q] * ga[c][q];
+              s[2 * r + 1] += g[q] * ga[c][q] * xh;
+            }
+          }
+        }
+      }
+    }
+    // two places by turns: a wave may be a round ahead of another's reads
+    row_sums<W>(s, red[turn], w, lane);
+    turn ^= 1;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (t0 + r < T) {
+        const float m1 = s[2 * r] / fd, m2 = s[2 * r + 1] / fd;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          const int at = (c * W + w) * 64 + lane;
+          float f[8], g[8];
+          unpack8(a[r][c], g);
+          unpack8(b[r][c], f);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            const float xh = (f[q] - mu[r]) * rs[r];
+            f[q] = (g[q] * ga[c][q] - m1 - xh * m2) * rs[r];
+          }
+          if constexpr (DH) {
+            unpack8(e[r][c], g);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f[q] += g[q];
+          }
+          if (at < nch) reinterpret_cast<uint4*>(dx + (t0 + r) * d)[at] = pack8(f);
+        }
+      }
+    }
+  }
+  float* p = part + static_cast<int64_t>(blockIdx.x) * 2 * d;
+  if constexpr (G == 1) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int at = (c * W + w) * 64 + lane;
+      if (at < nch)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          p[8 * at + q] = dg[c][q];
+          p[d + 8 * at + q] = db[c][q];
+        }
+    }
+  } else {
+    // the teams' sums, in their order
+    static_assert(W == 1, "a team's columns are those of one wave");
+    __shared__ float sums[G][C * 64 * 8];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (k) __syncthreads();
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          sums[team][(c * 64 + lane) * 8 + q] = k ? db[c][q] : dg[c][q];
+      __syncthreads();
+      for (int i = threadIdx.x; i < d; i += 256) {
+        float v = sums[0][i];
+#pragma unroll
+        for (int g = 1; g < G; ++g) v += sums[g][i];
+        p[k * d + i] = v;
+      }
+    }
+  }
+}
+
+// Rows beyond the registers' reach (d > NORM_HELD): a workgroup of 16 waves walks
+// its row again for each sum (its second and third passes come from the caches).
+template <bool RES>
+__global__ __launch_bounds__(1024) void norm_fwd_long_kernel(
+    const uint16_t* __restrict__ x, const uint16_t* __restrict__ res,
+    const float* __restrict__ gamma, const float* __restrict__ beta, int64_t T, int d, float eps,
+    uint16_t* __restrict__ h, uint16_t* __restrict__ y, float* __restrict__ mean,
+    float* __restrict__ rstd) {
+  __shared__ float red[2][16];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nch = d >> 3;
+  const float fd = static_cast<float>(d);
+  for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
+    const uint4* row = reinterpret_cast<const uint4*>(x + t * d);
+    float s[1] = {0.0f}, sq[1] = {0.0f}, f[8];
+    for (int c = threadIdx.x; c < nch; c += 1024) {
+      uint4 v = row[c];
+      if constexpr (RES) {
+        v = add8(v, reinterpret_cast<const uint4*>(res + t * d)[c]);
+        reinterpret_cast<uint4*>(h + t * d)[c] = v;
+      }
+      unpack8(v, f);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s[0] += f[q];
+    }
+    // each thread reads again what it wrote itself
+    if constexpr (RES) row = reinterpret_cast<const uint4*>(h + t * d);
+    row_sums<16>(s, red[0], w, lane);
+    const float mu = s[0] / fd;
+    for (int c = threadIdx.x; c < nch; c += 1024) {
+      unpack8(row[c], f);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) sq[0] += (f[q] - mu) * (f[q] - mu);
+    }
+    row_sums<16>(sq, red[1], w, lane);
+    const float rs = 1.0f / sqrtf(sq[0] / fd + eps);
+    for (int c = threadIdx.x; c < nch; c += 1024) {
+      float ga[8], be[8];
+      unpack8(row[c], f);
+      load8f(gamma + 8 * c, ga);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) be[q] = 0.0f;
+      if (beta) load8f(beta + 8 * c, be);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) f[q] = (f[q] - mu) * rs * ga[q] + be[q];
+      reinterpret_cast<uint4*>(y + t * d)[c] = pack8(f);
+    }
+    if (threadIdx.x == 0) {
+      if (mean) mean[t] = mu;
+      if (rstd) rstd[t] = rs;
+    }
+  }
+}
+
+template <bool DH>
+__global__ __launch_bounds__(1024) void norm_bwd_long_kernel(
+    const uint16_t* __restrict__ dy, const uint16_t* __restrict__ h,
+    const float* __restrict__ gamma, const float* __restrict__ mean,
+    const float* __restrict__ rstd, const uint16_t* __restrict__ dh, int64_t T, int d,
+    uint16_t* __restrict__ dx) {
+  __shared__ float red[2][32];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nch = d >> 3;
+  const float fd = static_cast<float>(d);
+  int turn = 0;
+  for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
+    const uint4* row = reinterpret_cast<const uint4*>(h + t * d);
+    const uint4* up = reinterpret_cast<const uint4*>(dy + t * d);
+    const float mu = mean[t], rs = rstd[t];
+    float s[2] = {0.0f, 0.0f}, f[8], g[8], ga[8];
+    for (int c = threadIdx.x; c < nch; c += 1024) {
+      unpack8(row[c], f);
+      unpack8(up[c], g);
+      load8f(gamma + 8 * c, ga);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        s[0] += g[q] * ga[q];
+        s[1] += g[q] * ga[q] * ((f[q] - mu) * rs);
+      }
+    }
+    row_sums<16>(s, red[turn], w, lane);
+    turn ^= 1;
+    const float m1 = s[0] / fd, m2 = s[1] / fd;
+    for (int c = threadIdx.x; c < nch; c += 1024) {
+      unpack8(row[c], f);
+      unpack8(up[c], g);
+      load8f(gamma + 8 * c, ga);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) f[q] = (g[q] * ga[q] - m1 - (f[q] - mu) * rs * m2) * rs;
+      if constexpr (DH) {
+        unpack8(reinterpret_cast<const uint4*>(dh + t * d)[c], g);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) f[q] += g[q];
+      }
+      reinterpret_cast<uint4*>(dx + t * d)[c] = pack8(f);
+    }
+  }
+}
+// Its weights' gradients: a wave sums 512 columns over a part of the rows.
+__global__ __launch_bounds__(256) void norm_cols_kernel(
+    const uint16_t* __restrict__ dy, const uint16_t* __restrict__ h,
+    const float* __restrict__ mean, const float* __restrict__ rstd, int64_t T, int d, int64_t rows,
+    float* __restrict__ part) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int c = (blockIdx.x * 4 + w) * 64 + lane;
+  if (c >= d >> 3) return;
+  float dg[8] = {}, db[8] = {}, f[8], g[8];
+  const int64_t t1 = min(T, (blockIdx.y + 1) * rows);
+  for (int64_t t = blockIdx.y * rows; t < t1; ++t) {
+    unpack8(reinterpret_cast<const uint4*>(h + t * d)[c], f);
+    unpack8(reinterpret_cast<const uint4*>(dy + t * d)[c], g);
+    const float mu = mean[t], rs = rstd[t];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      dg[q] += g[q] * ((f[q] - mu) * rs);
+      db[q] += g[q];
+    }
+  }
+  float* p = part + static_cast<int64_t>(blockIdx.y) * 2 * d + 8 * c;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    p[q] = dg[q];
+    p[d + q] = db[q];
+  }
+}
+
+// out[i] = sum over parts of part[p][i]: 64 columns a workgroup, its 4 waves take
+// every fourth part (joined in order), dgamma then dbeta (null: not wanted).
+__global__ __launch_bounds__(256) void norm_sum_kernel(const float* __restrict__ part, int parts,
+                                                       int d, float* __restrict__ dgamma,
+                                                       float* __restrict__ dbeta) {
+  __shared__ float sums[4][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+  float s = 0.0f;
+  if (i < 2 * d) {
+    int p = w;
+    for (; p + 28 < parts; p += 32) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = part[static_cast<int64_t>(p + 4 * u) * 2 * d + i];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s += v[u];
+    }
+    for (; p < parts; p += 4) s += part[static_cast<int64_t>(p) * 2 * d + i];
+  }
+  sums[w][lane] = s;
+  __syncthreads();
+  if (w == 0 && i < 2 * d) {
+    s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    if (i < d)
+      dgamma[i] = s;
+    else if (dbeta)
+      dbeta[i - d] = s;
+  }
+}
+
+constexpr int NORM_HELD = 16384;  // widest row held in registers
+
+// Workgroups of a backward pass: what is resident, less where each would have
+// few rows (their partial sums, 8 bytes a column, weigh against 6 a row's).
+int64_t bwd_groups(int64_t T, int d) {
+  if (d > NORM_HELD) return std::clamp<int64_t>(T / 64, 1, 64);
+  const int64_t teams = d <= 1024 ? 4 : 1;
+  return std::clamp<int64_t>(ceil_div(T, 4 * teams), 1, d <= 4096 ? 768 : d <= 8192 ? 512 : 256);
+}
+
+template <typename F>
+void by_width(int d, F&& f) {
+  using std::integral_constant;
+  if (d <= 512) f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+  else if (d <= 1024) f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
+  else if (d <= 2048) f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+  else if (d <= 4096) f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+  else if (d <= 8192) f(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+  else f(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+}
+
+}  // namespace
+
+hipError_t launch_norm_fwd(const uint16_t* x, const uint16_t* res, const float* gamma,
+                           const float* beta, int64_t T, int d, float eps, uint16_t* h,
+                           uint16_t* y, float* mean, float* rstd, hipStream_t s) {
+  if (T == 0) return hipSuccess;
+  prof_begin(K_NORM_FWD, s);
+  if (d > NORM_HELD) {
+    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(T, 2 * device_cus()));
+    if (res)
+      norm_fwd_long_kernel<true><<<grid, 1024, 0, s>>>(x, res, gamma, beta, T, d, eps, h, y, mean, rstd);
+    else
+      norm_fwd_long_kernel<false><<<grid, 1024, 0, s>>>(x, res, gamma, beta, T, d, eps, h, y, mean, rstd);
+  } else {
+    by_width(d, [&](auto w, auto c) {
+      constexpr int W = w, C = c, G = W < 4 ? 4 / W : 1, threads = W < 4 ? 256 : 64 * W;
+      const unsigned grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(T, G), 8 * device_cus()));
+      if (res)
+        norm_fwd_kernel<W, C, 1, true><<<grid, threads, 0, s>>>(x, res, gamma, beta, T, d, eps, h, y, mean, rstd);
+      else
+        norm_fwd_kernel<W, C, 1, false><<<grid, threads, 0, s>>>(x, res, gamma, beta, T, d, eps, h, y, mean, rstd);
+    });
+  }
+  prof_end(K_NORM_FWD, s);
+  return hipGetLastError();
+}
+
+size_t norm_bwd_ws_bytes(int64_t T, int d) {
+  return align_up(sizeof(float) * 2 * static_cast<size_t>(bwd_groups(T, d)) * d, 256);
+}
+
+hipError_t launch_norm_bwd(const uint16_t* dy, const uint16_t* h, const float* gamma,
+                           const float* mean, const float* rstd, const uint16_t* dh, int64_t T,
+                           int d, uint16_t* dx, float* dgamma, float* dbeta, void* ws,
+                           hipStream_t s) {
+  float* part = static_cast<float*>(ws);
+  const int64_t groups = T == 0 ? 0 : bwd_groups(T, d);
+  if (T > 0) {
+    prof_begin(K_NORM_BWD, s);
+    if (d > NORM_HELD) {
+      const unsigned grid = static_cast<unsigned>(std::min<int64_t>(T, 2 * device_cus()));
+      if (dh)
+        norm_bwd_long_kernel<true><<<grid, 1024, 0, s>>>(dy, h, gamma, mean, rstd, dh, T, d, dx);
+      else
+        norm_bwd_long_kernel<false><<<grid, 1024, 0, s>>>(dy, h, gamma, mean, rstd, dh, T, d, dx);
+      const dim3 cols(static_cast<unsigned>(ceil_div(d, 2048)), static_cast<unsigned>(groups));
+      norm_cols_kernel<<<cols, 256, 0, s>>>(dy, h, mean, rstd, T, d, ceil_div(T, groups), part);
+    } else {
+      by_width(d, [&](auto w, auto c) {
+        constexpr int W = w, C = c, threads = W < 4 ? 256 : 64 * W;
+        const unsigned grid = static_cast<unsigned>(groups);
+        if (dh)
+          norm_bwd_kernel<W, C, 1, true><<<grid, threads, 0, s>>>(dy, h, gamma, mean, rstd, dh, T, d, dx, part);
+        else
+          norm_bwd_kernel<W, C, 1, false><<<grid, threads, 0, s>>>(dy, h, gamma, mean, rstd, dh, T, d, dx, part);
+      });
+    }
+    prof_end(K_NORM_BWD, s);
+  }
+  prof_begin(K_NORM_SUM, s);
+  norm_sum_kernel<<<static_cast<unsigned>(ceil_div(2 * static_cast<int64_t>(d), 64)), 256, 0, s>>>(
+      part, static_cast<int>(groups), d, dgamma, dbeta);
+  prof_end(K_NORM_SUM, s);
+  return hipGetLastError();
+}
+
+}  // namespace moe

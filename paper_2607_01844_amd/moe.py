@@ -13,8 +13,9 @@ import functools
 
 import torch
 
-from ._abi import (C_SYMBOLS, LIB_PATH, MOE_BWD_DGRAD, MOE_BWD_WGRAD, MOE_MAX_DIM,  # noqa: F401
-                   MOE_MAX_E, MOE_MAX_K, MOE_OK, MOE_PERMUTE_NOALLOC_MAX_BYTES, MoEError)
+from ._abi import (C_SYMBOLS, LIB_PATH, MOE_BF16, MOE_BWD_DGRAD, MOE_BWD_WGRAD,  # noqa: F401
+                   MOE_F32, MOE_MAX_DIM, MOE_MAX_E, MOE_MAX_K, MOE_OK,
+                   MOE_PERMUTE_NOALLOC_MAX_BYTES, AdamWOptions, MoEError, Param)
 from ._abi import load as _load
 
 lib = _load()
@@ -647,6 +648,287 @@ def moe_vocab_distill_bwd(x, w_voc, topk_idx, topk_logit, lse, y_topk, dloss, vb
                                      _ptr(dloss), N, H, V, vblock, K, _ptr(dx), _ptr(dw_voc),
                                      _ptr(ws), ws.numel(), _stream()), "moe_vocab_distill_bwd")
     return dx, dw_voc
+
+
+# --------------------------------------------------------------- embedding
+def moe_embedding_fwd(ids, w, scale=1.0, vocab_begin=0, y=None):
+    """Rows of w [rows,H] bf16 (vocabulary entries [vocab_begin, vocab_begin +
+    rows)) for ids [N] int32, times scale; zeros for ids outside them (another
+    rank's, or -1 for padding).  Returns y [N,H] bf16."""
+    _need(w, torch.bfloat16, "w", 2)
+    _need(ids, torch.int32, "ids", 1)
+    rows, H = _given(w, torch.bfloat16, "w", w.shape).shape
+    N = _given(ids, torch.int32, "ids", ids.shape).shape[0]
+    y = _out(y, torch.bfloat16, "y", (N, H), w.device)
+    _check(lib.moe_embedding_fwd(_ptr(ids), _ptr(w), N, H, vocab_begin, rows, scale, _ptr(y),
+                                 _stream()), "moe_embedding_fwd")
+    return y
+
+
+def moe_embedding_bwd(ids, dy, rows, scale=1.0, vocab_begin=0, dw=None):
+    """Gradient of the embedding's weights from dy [N,H] bf16: dw [rows,H] bf16,
+    every row written (zeros where no token named it)."""
+    _need(dy, torch.bfloat16, "dy", 2)
+    N, H = _given(dy, torch.bfloat16, "dy", dy.shape).shape
+    _given(ids, torch.int32, "ids", (N,))
+    ws = workspace(_ws_bytes("moe_embedding_bwd_workspace_bytes", N, H, rows), dy.device,
+                   "embedding_bwd")
+    dw = _out(dw, torch.bfloat16, "dw", (rows, H), dy.device)
+    _check(lib.moe_embedding_bwd(_ptr(ids), _ptr(dy), N, H, vocab_begin, rows, scale, _ptr(dw),
+                                 _ptr(ws), ws.numel(), _stream()), "moe_embedding_bwd")
+    return dw
+
+
+# -------------------------------------------------------------- layer norm
+def moe_layer_norm_fwd(x, gamma, beta=None, eps=1e-5, residual=None, y=None, h=None, stats=True):
+    """Layer norm of h = x + residual (rounded to bf16; h is x without a
+    residual), rows [T,d] bf16, gamma and beta [d] fp32.  Returns (y, h, mean
+    [T], rstd [T]); stats=False: None in the place of the last two."""
+    _need(x, torch.bfloat16, "x", 2)
+    T, d = _given(x, torch.bfloat16, "x", x.shape).shape
+    _given(gamma, torch.float32, "gamma", (d,))
+    if beta is not None:
+        _given(beta, torch.float32, "beta", (d,))
+    dev = x.device
+    if residual is not None:
+        _given(residual, torch.bfloat16, "residual", (T, d))
+        h = _out(h, torch.bfloat16, "h", (T, d), dev)
+    elif h is not None:
+        raise ValueError("h is an output of a residual sum: without residual it is x")
+    y = _out(y, torch.bfloat16, "y", (T, d), dev)
+    mean = torch.empty((T,), dtype=torch.float32, device=dev) if stats else None
+    rstd = torch.empty((T,), dtype=torch.float32, device=dev) if stats else None
+    _check(lib.moe_layer_norm_fwd(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), T, d, eps,
+                                  _ptr(h), _ptr(y), _ptr(mean), _ptr(rstd), _stream()),
+           "moe_layer_norm_fwd")
+    return y, x if residual is None else h, mean, rstd
+
+
+def moe_layer_norm_bwd(dy, h, gamma, mean, rstd, dh=None, dx=None, with_dbeta=True):
+    """Gradients of the layer norm from dy [T,d] and the forward's h, mean and
+    rstd; dh [T,d]: the gradient that reaches h by another way (the residual
+    stream's), added to dx.  Returns (dx [T,d] bf16, dgamma [d], dbeta [d] or
+    None, fp32); dx is the gradient of x and of the residual alike."""
+    _need(h, torch.bfloat16, "h", 2)
+    T, d = _given(h, torch.bfloat16, "h", h.shape).shape
+    _given(dy, torch.bfloat16, "dy", (T, d))
+    _given(gamma, torch.float32, "gamma", (d,))
+    _given(mean, torch.float32, "mean", (T,))
+    _given(rstd, torch.float32, "rstd", (T,))
+    if dh is not None:
+        _given(dh, torch.bfloat16, "dh", (T, d))
+    dev = h.device
+    ws = workspace(_ws_bytes("moe_layer_norm_bwd_workspace_bytes", T, d), dev, "layer_norm_bwd")
+    dx = _out(dx, torch.bfloat16, "dx", (T, d), dev)
+    dgamma = torch.empty((d,), dtype=torch.float32, device=dev)
+    dbeta = torch.empty((d,), dtype=torch.float32, device=dev) if with_dbeta else None
+    _check(lib.moe_layer_norm_bwd(_ptr(dy), _ptr(h), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dh),
+                                  T, d, _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), ws.numel(),
+                                  _stream()), "moe_layer_norm_bwd")
+    return dx, dgamma, dbeta
+
+
+# ---------------------------------------------------------- weight updates
+_TYPES = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}
+STATE_BLOCK = 128  # elements of one scale of an 8-bit state
+
+
+class Params:
+    """The tensors of a weight update, checked once and kept: weights w (fp32 or
+    bf16), gradients g (fp32 or bf16), states m and v, and optionally bf16 copies
+    of fp32 weights that each step writes (w_copy; None where a weight has none).
+    Lists of the same length; tensors of any shape, contiguous, of equal sizes.
+    A state is an fp32 tensor, or in 8 bits a pair (codes [n] uint8, scales
+    [ceil(n / 128)] uint8); without m and v they start as zeros, in `bits` bits.
+    w=None: gradients alone, for moe_grad_sumsq.  The tensors stay alive as long as
+    this does, and gradients are read from where they are at every step
+    (`set_grads` names others)."""
+
+    def __init__(self, w, g, m=None, v=None, w_copy=None, bits=None):
+        self.g = list(g)
+        self.count = count = len(self.g)
+        self.device = None
+        self.array = (Param * max(count, 1))()
+        self.w = None if w is None else list(w)
+        self.w_copy = [None] * count if w_copy is None else list(w_copy)
+        self.m, self.v, self.bits = m, v, bits
+        sized, name = (self.g, "g") if w is None else (self.w, "w")
+        for i, t in enumerate(sized):
+            if not isinstance(t, torch.Tensor):
+                raise ValueError(f"{name}[{i}] is required")
+        sizes = [t.numel() for t in sized]
+        spans = []
+        if w is None:
+            if m is not None or v is not None or w_copy is not None or bits is not None:
+                raise ValueError("states and copies need weights")
+        else:
+            if len(self.w) != count or len(self.w_copy) != count:
+                raise ValueError("w, g and w_copy need one entry for each tensor")
+            if (m is None) != (v is None):
+                raise ValueError("m and v come together")
+            if m is None:
+                self._new_states(sizes, 32 if bits is None else bits)
+            else:
+                self._given_states(m, v, bits)
+            for i, (p, n) in enumerate(zip(self.array, sizes)):
+                p.w, p.w_type = self._take(self.w[i], tuple(_TYPES), f"w[{i}]", n, spans)
+                if self.w_copy[i] is not None:
+                    if p.w_type != MOE_F32:
+                        raise TypeError(f"w_copy[{i}]: only fp32 weights have a copy")
+                    p.w_copy, _ = self._take(self.w_copy[i], (torch.bfloat16,), f"w_copy[{i}]", n,
+                                             spans)
+                for name, state in (("m", self.m[i]), ("v", self.v[i])):
+                    at = f"{name}[{i}]"
+                    if self.bits == 32:
+                        a, _ = self._take(state, (torch.float32,), at, n, spans)
+                    else:
+                        codes, scales = state
+                        a, _ = self._take(codes, (torch.uint8,), at, n, spans)
+                        b, _ = self._take(scales, (torch.uint8,), at + " scales",
+                                          -(-n // STATE_BLOCK), spans)
+                        setattr(p, name + "_scale", b)
+                    setattr(p, name, a)
+        self.sizes = sizes
+        self._written = spans
+        self.set_grads(self.g)
+
+    def _new_states(self, sizes, bits):
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        self.bits = bits
+
+        def zeros(i, n):
+            dev = self.w[i].device
+            if bits == 32:
+                return torch.zeros((n,), dtype=torch.float32, device=dev)
+            return (torch.zeros((n,), dtype=torch.uint8, device=dev),
+                    torch.zeros((-(-n // STATE_BLOCK),), dtype=torch.uint8, device=dev))
+        self.m = [zeros(i, n) for i, n in enumerate(sizes)]
+        self.v = [zeros(i, n) for i, n in enumerate(sizes)]
+
+    def _given_states(self, m, v, bits):
+        self.m, self.v = list(m), list(v)
+        if len(self.m) != self.count or len(self.v) != self.count:
+            raise ValueError("m and v need one entry for each tensor")
+        pairs = {isinstance(t, (tuple, list)) for t in self.m + self.v}
+        if len(pairs) > 1:
+            raise ValueError("states are all in 32 bits or all in 8")
+        held = 8 if pairs == {True} else 32 if pairs else bits or 32
+        if bits is not None and bits != held:
+            raise ValueError(f"states are in {held} bits, not in {bits}")
+        self.bits = held
+
+    def _take(self, t, dtypes, name, n, spans):
+        """(address, type) of a tensor of n elements; its span joins `spans`."""
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{name} is required")
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name}: expected {' or '.join(map(str, dtypes))}, got {t.dtype}")
+        if not t.is_cuda:
+            raise TypeError(f"{name} must be a device tensor")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if t.numel() != n:
+            raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
+        if self.device is None:
+            self.device = t.get_device()
+        if t.get_device() != self.device:
+            raise ValueError(f"{name} is on {t.device}, not on the other tensors' device")
+        if n:
+            spans.append((t.data_ptr(), t.data_ptr() + n * t.element_size(), name))
+        return t.data_ptr(), _TYPES.get(t.dtype, 0)
+
+    def set_grads(self, g):
+        """Other gradient tensors, one for each weight."""
+        g = list(g)
+        if len(g) != self.count:
+            raise ValueError("g needs one entry for each tensor")
+        read = []
+        at = [self._take(t, tuple(_TYPES), f"g[{i}]", n, read)
+              for i, (t, n) in enumerate(zip(g, self.sizes))]
+        # what a step writes lies apart from all else that it reads or writes
+        spans = sorted([s + (True,) for s in self._written] + [s + (False,) for s in read])
+        last, last_written = (0, 0, None), (0, 0, None)  # the spans that reach furthest
+        for s in spans:
+            over = last if s[3] else last_written
+            if s[0] < over[1]:
+                raise ValueError(f"{s[2]} overlaps {over[2]}")
+            last = max(last, s, key=lambda x: x[1])
+            if s[3]:
+                last_written = max(last_written, s, key=lambda x: x[1])
+        for p, n, (a, kind) in zip(self.array, self.sizes, at):
+            p.g, p.g_type, p.n = a, kind, n
+        self.g = g
+        need = ctypes.c_size_t()
+        _check(lib.moe_grad_sumsq_workspace_bytes(self.array, self.count, ctypes.byref(need)),
+               "moe_grad_sumsq_workspace_bytes")
+        self.sumsq_bytes = need.value
+
+    def on_device(self):
+        """Refuses a current device that is not the tensors' own."""
+        if self.device is not None and self.device != torch._C._cuda_getDevice():
+            raise ValueError(f"the tensors are on cuda:{self.device}, not on the current device")
+        return self
+
+
+def moe_grad_sumsq(params, sumsq=None):
+    """Sum of squares of all gradients of `params` (a Params, or a list of bf16
+    and fp32 tensors).  Returns sumsq [1] fp32; ranks that hold parts of a model
+    add theirs up before moe_adamw_step clips by it."""
+    if not isinstance(params, Params):
+        params = Params(None, params)
+    params.on_device()
+    dev = torch._C._cuda_getDevice()
+    sumsq = _out(sumsq, torch.float32, "sumsq", (1,), f"cuda:{dev}")
+    ws = workspace(params.sumsq_bytes, dev, "grad_sumsq")
+    _check(lib.moe_grad_sumsq(params.array, params.count, _ptr(sumsq), _ptr(ws), ws.numel(),
+                              _stream()), "moe_grad_sumsq")
+    return sumsq
+
+
+def _number(v, dtype, name):
+    """(host number or 0, address or None) of a number or a device scalar [1]."""
+    if isinstance(v, torch.Tensor):
+        return 0, _given(v, dtype, name, (1,)).data_ptr()
+    return v, None
+
+
+def moe_adamw_step(params, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1,
+                   grad_sumsq=None, max_norm=float("inf"), seed=0):
+    """One AdamW step of all tensors of `params`, in place.  lr and step (1 for the
+    first) are numbers, or device tensors [1] (fp32, int32) that a captured step
+    reads at every replay.  grad_sumsq [1] fp32: gradients are clipped to a norm of
+    max_norm by it, and a step with a sum that is not finite is left out.  seed: of
+    the random rounding of 8-bit states and of bf16 weights (with the step)."""
+    params.on_device()
+    if params.w is None:
+        raise ValueError("these params have no weights")
+    if grad_sumsq is not None:
+        _given(grad_sumsq, torch.float32, "grad_sumsq", (1,))
+    lr, lr_device = _number(lr, torch.float32, "lr")
+    step, step_device = _number(step, torch.int32, "step")
+    o = AdamWOptions(lr, beta1, beta2, eps, weight_decay, step, lr_device, step_device,
+                     _ptr(grad_sumsq), max_norm, seed & 0xFFFFFFFF)
+    _check(lib.moe_adamw_step(params.array, params.count, params.bits, ctypes.byref(o), _stream()),
+           "moe_adamw_step")
+
+
+def moe_adamw_states(params, m=None, v=None):
+    """The values of 8-bit states: two lists of fp32 tensors [n] (m, v: given ones
+    to write)."""
+    params.on_device()
+    if params.w is None or params.bits != 8:
+        raise ValueError("these params have no 8-bit states")
+    out = []
+    for name, given in (("m", m), ("v", v)):
+        given = [None] * params.count if given is None else list(given)
+        if len(given) != params.count:
+            raise ValueError(f"{name} needs one entry for each tensor")
+        out.append([_out(t, torch.float32, f"{name}[{i}]", (n,), f"cuda:{params.device}")
+                    for i, (t, n) in enumerate(zip(given, params.sizes))])
+    at = [(ctypes.c_void_p * max(params.count, 1))(*[t.data_ptr() for t in o]) for o in out]
+    _check(lib.moe_adamw_states(params.array, params.count, *at, _stream()), "moe_adamw_states")
+    return tuple(out)
 
 
 # ------------------------------------------ least-loaded expert parallelism

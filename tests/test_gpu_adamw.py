@@ -1,0 +1,309 @@
+"""The gradients' sum of squares and the AdamW step on the GPU: values against 64
+bits, 8-bit states bit for bit against 32-bit arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+from tests import train_step_ref as R
+
+pytestmark = pytest.mark.gpu
+
+HYPER = dict(lr=3e-3, beta1=0.9, beta2=0.95, eps=1e-8, weight_decay=0.1)
+# one element, ends of groups of 4, of blocks of 128, of a workgroup's piece, empty ones
+SIZES = [1, 3, 4, 5, 127, 128, 129, 0, 1000, 2047, 2048, 2049, 16384, 16385, 33333]
+
+
+def make(sizes, seed, bits, w_types, g_types, copies=True, history=True):
+    g = torch.Generator().manual_seed(seed)
+    out = {"w": [], "g": [], "m": [], "v": [], "copy": []}
+    for i, n in enumerate(sizes):
+        wt, gt = w_types[i % len(w_types)], g_types[i % len(g_types)]
+        out["w"].append((0.1 * torch.randn(n, generator=g)).to(wt))
+        out["g"].append((torch.randn(n, generator=g) * torch.exp(2 * torch.randn(n, generator=g)) * 1e-2).to(gt))
+        m = 1e-2 * torch.randn(n, generator=g) * torch.exp(2 * torch.randn(n, generator=g))
+        v = 1e-4 * torch.exp(3 * torch.randn(n, generator=g))
+        if not history:
+            m, v = 0 * m, 0 * v
+        if bits == 8:
+            half = np.full(n, 1 << 15)
+            m, v = ([torch.from_numpy(a) for a in R.encode(x.numpy(), k, half)]
+                    for x, k in ((m, "m"), (v, "v")))
+        out["m"].append(m)
+        out["v"].append(v)
+        out["copy"].append(torch.zeros(n, dtype=torch.bfloat16) if copies and wt is torch.float32
+                           and i % 3 else None)
+    return out
+
+
+def cuda(t):
+    if t is None:
+        return None
+    return tuple(x.cuda() for x in t) if isinstance(t, (list, tuple)) else t.cuda()
+
+
+def on_gpu(t, moe):
+    c = {k: [cuda(x) for x in v] for k, v in t.items()}
+    return moe.Params(c["w"], c["g"], c["m"], c["v"], c["copy"])
+
+
+def values(t, i, kind, bits):
+    x = t[kind][i]
+    return R.decode(x[0].numpy(), x[1].numpy(), kind) if bits == 8 else x.numpy()
+
+
+def clip_of(sumsq, max_norm):
+    if sumsq is None:
+        return 1.0
+    n = float(np.sqrt(np.float64(np.float32(sumsq))))
+    return max_norm / n if n > max_norm else 1.0
+
+
+def check(t, params, bits, step, sumsq, max_norm, seed, first=0):
+    """Every tensor of the params after one step from the tensors t."""
+    h = HYPER
+    clip = clip_of(sumsq, max_norm)
+    u = R.U
+    for i, w in enumerate(t["w"]):
+        n = w.numel()
+        m0, v0 = (torch.from_numpy(values(t, i, k, bits).copy()).double() for k in "mv")
+        g = t["g"][i].double()
+        w1, m1, v1 = R.adamw(w.double(), g, m0, v0, h["lr"], step, h["beta1"], h["beta2"], h["eps"],
+                             h["weight_decay"], clip)
+        em = 5 * u * (h["beta1"] * m0.abs() + (1 - h["beta1"]) * (g * clip).abs()) + 1e-44
+        ev = 7 * u * v1 + 1e-44
+        if bits == 32:
+            assert ((R.f64(params.m[i]) - m1).abs() <= em).all(), i
+            assert ((R.f64(params.v[i]) - v1).abs() <= ev).all(), i
+        else:
+            # the same operations in numpy, every one rounded
+            m32, v32 = R.states32(values(t, i, "m", 8), values(t, i, "v", 8),
+                                  t["g"][i].float().numpy(), h["beta1"], h["beta2"], np.float32(clip))
+            r = R.random_bits(n, seed, step, first + i)
+            for kind, x, r16 in (("m", m32, r & np.uint64(0xFFFF)), ("v", v32, r >> np.uint64(16))):
+                codes, scales = R.encode(x, kind, r16)
+                got = getattr(params, kind)[i]
+                assert np.array_equal(got[1].cpu().numpy(), scales), (i, kind)
+                assert np.array_equal(got[0].cpu().numpy(), codes), (i, kind)
+        # the quotient: its numerator's error, a root, a product, a sum, a division
+        bc1, bc2 = 1 - h["beta1"] ** step, 1 - h["beta2"] ** step
+        den = torch.sqrt(v1 / bc2) + h["eps"]
+        rate = h["lr"] / bc1
+        # (1e-22: the root of what is lost of v' below the normal numbers)
+        q = (m1 / den).abs()
+        tol = u * (4 * w.double().abs() + 18 * rate * q) + rate * em / den + \
+            rate * q * 1e-22 / den + 2 * u * w1.abs()
+        got = R.f64(params.w[i])
+        if w.dtype is torch.float32:
+            assert ((got - w1).abs() <= 1.01 * tol).all(), i
+            if t["copy"][i] is not None:
+                assert torch.equal(params.w_copy[i].cpu(), params.w[i].cpu().bfloat16())
+        else:
+            # rounded by known random bits: from the ends of what w' can be
+            r = R.random_bits(n, seed, step, first + i)
+            rw = (r * np.uint64(0xBB67AE85) & np.uint64(0xFFFFFFFF)) >> np.uint64(16)
+            ends = []
+            for s in (-1.01, 1.01):
+                b = (w1 + s * tol).float().numpy().view(np.uint32).astype(np.int64) + rw.astype(np.int64)
+                ends.append((b & 0xFFFF0000).astype(np.uint32).view(np.float32).astype(np.float64))
+            lo, hi = (np.minimum(*ends), np.maximum(*ends))
+            x = got.numpy()
+            assert ((x >= lo) & (x <= hi)).all(), i
+
+
+F32, BF = torch.float32, torch.bfloat16
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("w_types,g_types", [((F32,), (BF,)), ((BF,), (F32,)), ((F32, BF), (BF, F32, BF))],
+                         ids=["fp32", "bf16", "mixed"])
+@pytest.mark.parametrize("clip", [None, 0.5, 1e30])
+def test_step(bits, w_types, g_types, clip):
+    from paper_2607_01844_amd import moe
+    print(bits, w_types, g_types, clip, flush=True)
+    t = make(SIZES, 1, bits, w_types, g_types)
+    p = on_gpu(t, moe)
+    s = None if clip is None else 7.7
+    q = None if s is None else torch.tensor([s], device="cuda")
+    moe.moe_adamw_step(p, step=9, grad_sumsq=q, max_norm=clip or 1.0, seed=123, **HYPER)
+    check(t, p, bits, 9, s, clip or 1.0, 123)
+    if bits == 8:
+        m, v = moe.moe_adamw_states(p)
+        for kind, vals in (("m", m), ("v", v)):
+            for x, (c, s8) in zip(vals, getattr(p, kind)):
+                assert np.array_equal(x.cpu().numpy(), R.decode(c.cpu().numpy(), s8.cpu().numpy(), kind))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_first_steps_from_zero_states(bits):
+    from paper_2607_01844_amd import moe
+    sizes = [300, 5000]
+    t = make(sizes, 2, bits, (F32,), (BF,), history=False)
+    c = {k: [cuda(x) for x in t[k]] for k in ("w", "g", "copy")}
+    p = moe.Params(c["w"], c["g"], w_copy=c["copy"], bits=bits)
+    for step in (1, 2, 3):
+        moe.moe_adamw_step(p, step=step, seed=5, **HYPER)
+        check(t, p, bits, step, None, 1.0, 5)
+        for k in "mv":
+            t[k] = [tuple(y.cpu() for y in x) if bits == 8 else x.cpu() for x in getattr(p, k)]
+        t["w"] = [x.cpu() for x in p.w]
+
+
+def test_many_tensors_in_several_launches():
+    from paper_2607_01844_amd import moe
+    sizes = [(i * 37) % 300 for i in range(131)] + [0, 0, 5, 0]
+    for bits in (32, 8):
+        t = make(sizes, 3, bits, (F32, BF), (BF, F32, F32), copies=False)
+        p = on_gpu(t, moe)
+        moe.moe_adamw_step(p, step=4, seed=77, **HYPER)
+        check(t, p, bits, 4, None, 1.0, 77)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_device_numbers_are_those_of_the_host(bits):
+    from paper_2607_01844_amd import moe
+    t = make([1, 500, 4097], 4, bits, (F32, BF), (BF,))
+    a, b = on_gpu(t, moe), on_gpu(t, moe)
+    h = dict(HYPER)
+    lr = torch.tensor([h.pop("lr")], device="cuda")
+    moe.moe_adamw_step(a, float(lr), 12, seed=1, **h)
+    moe.moe_adamw_step(b, lr, torch.tensor([12], dtype=torch.int32, device="cuda"), seed=1, **h)
+    for x, y in zip(a.w, b.w):
+        assert torch.equal(x, y)
+    for k in "mv":
+        for x, y in zip(getattr(a, k), getattr(b, k)):
+            for u, w in zip(x if bits == 8 else [x], y if bits == 8 else [y]):
+                assert torch.equal(u, w)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -1.0])
+def test_step_left_out(bits, bad):
+    from paper_2607_01844_amd import moe
+    t = make(SIZES, 6, bits, (F32, BF), (BF, F32))
+    p = on_gpu(t, moe)
+    moe.moe_adamw_step(p, step=3, grad_sumsq=torch.tensor([bad], device="cuda"), **HYPER)
+    for k, held in (("w", p.w), ("m", p.m), ("v", p.v), ("copy", p.w_copy)):
+        for x, y in zip(t[k], held):
+            for u, w in zip(x, y) if isinstance(x, (list, tuple)) else [(x, y)]:
+                assert u is None or torch.equal(u, w.cpu())
+
+
+def test_special_gradients_without_a_norm():
+    # a NaN or an infinity reaches its element (32 bits) or its block (8 bits)
+    from paper_2607_01844_amd import moe
+    n = 1000
+    for bits in (32, 8):
+        t = make([n], 8, bits, (F32,), (F32,))
+        t["g"][0][300], t["g"][0][700] = float("nan"), float("inf")
+        p = on_gpu(t, moe)
+        moe.moe_adamw_step(p, step=2, **HYPER)
+        m = moe.moe_adamw_states(p)[0][0] if bits == 8 else p.m[0]
+        bad = torch.zeros(n, dtype=torch.bool)
+        if bits == 32:
+            bad[300] = bad[700] = True
+        else:
+            bad[256:384] = bad[640:768] = True
+        assert torch.equal(~m.isfinite().cpu(), bad)
+        w = ~p.w[0].isfinite().cpu()
+        assert w[300] and w[700] and int(w.sum()) == 2
+
+
+def test_rows_behind_a_tensor_are_left():
+    from paper_2607_01844_amd import moe
+    n, room = 1001, 1408
+    for bits in (32, 8):
+        t = make([n], 10, bits, (F32,), (BF,))
+        t["copy"][0] = torch.zeros(n, dtype=BF)
+        wide = {}
+        for k in ("w", "g", "m", "v", "copy"):
+            for j, x in enumerate(t[k][0] if isinstance(t[k][0], (list, tuple)) else [t[k][0]]):
+                big = torch.full((room,), 7, dtype=x.dtype, device="cuda")
+                big[:x.numel()] = x.cuda()
+                wide[k, j] = (big, x.numel())
+        cut = {k: [tuple(wide[k, j][0][:wide[k, j][1]] for j in (0, 1)) if (k, 1) in wide else
+                   wide[k, 0][0][:n]] for k in ("w", "g", "m", "v", "copy")}
+        p = moe.Params(cut["w"], cut["g"], cut["m"], cut["v"], cut["copy"])
+        moe.moe_adamw_step(p, step=2, **HYPER)
+        for big, used in wide.values():
+            assert (big[used:] == 7).all()
+
+
+@pytest.mark.parametrize("types", [(BF,), (F32,), (BF, F32)], ids=["bf16", "fp32", "mixed"])
+def test_sumsq(types):
+    from paper_2607_01844_amd import moe
+    g = torch.Generator().manual_seed(11)
+    sizes = SIZES + [7, 100001] + [(i * 31) % 97 for i in range(100)] + [3000000]
+    grads = [torch.randn(n, generator=g).to(types[i % len(types)]) for i, n in enumerate(sizes)]
+    ref = sum(float(R.f64(x).square().sum()) for x in grads)
+    dev = [x.cuda() for x in grads]
+    got = moe.moe_grad_sumsq(dev)
+    # a square and 64 additions in 32 bits, 64 bits beyond, one rounding
+    assert abs(float(got) - ref) <= 66 * R.U * ref
+    assert torch.equal(got, moe.moe_grad_sumsq(moe.Params(None, dev)))
+    assert float(moe.moe_grad_sumsq([])) == 0 and float(moe.moe_grad_sumsq([dev[7]])) == 0
+    dev[0][0] = float("nan")
+    assert moe.moe_grad_sumsq(dev).isnan()
+    dev[0][0] = 1e30
+    assert moe.moe_grad_sumsq(dev).isinf()
+
+
+def test_mean_of_8_bit_states_follows_the_32_bit_ones():
+    # 60 steps of one gradient: rounded at random, the states' means over many
+    # elements go with those of 32 bits; to the nearest v would stand still
+    from paper_2607_01844_amd import moe
+    n = 1 << 16
+    g = torch.full((n,), 0.5, device="cuda")
+    p8 = moe.Params([torch.zeros(n, device="cuda")], [g], bits=8)
+    beta2 = 0.99
+    for step in range(1, 61):
+        moe.moe_adamw_step(p8, 0.0, step, 0.9, beta2, 1e-8, 0.0, seed=3)
+    v = moe.moe_adamw_states(p8)[1][0].double()
+    want = 0.25 * (1 - beta2 ** 60)
+    # each step adds an error of at most half a step (v / 16) in the root mean square,
+    # kept by beta2: six sigma over n elements, and the 2^-16 of a step that the random
+    # bits resolve, 60 times
+    sigma = want / 16 * 60 ** 0.5 / n ** 0.5
+    assert abs(float(v.mean()) - want) <= 6 * sigma + 60 * want / 8 * 2.0 ** -16
+
+
+def test_refusals():
+    from paper_2607_01844_amd import moe
+    z = lambda n, dt=F32: torch.zeros((n,), dtype=dt, device="cuda")  # noqa: E731
+    a, g = z(200), z(200, BF)
+    for bad in (lambda: moe.Params([a.half()], [g]), lambda: moe.Params([a.cpu()], [g]),
+                lambda: moe.Params([g], [a], w_copy=[z(200, BF)]), lambda: moe.Params([a], [g.long()]),
+                lambda: moe.Params([a], [g], [z(200, BF)], [z(200)])):
+        with pytest.raises(TypeError):
+            bad()
+    codes, scales = z(200, torch.uint8), z(2, torch.uint8)
+    for bad in (lambda: moe.Params([a], [g, g]), lambda: moe.Params([a], [z(199)]), lambda: moe.Params([None], [g]),
+                lambda: moe.Params([a[::2]], [g[:100]]), lambda: moe.Params([a], [g], [z(200)], None),
+                lambda: moe.Params([a], [g], [z(199)], [z(200)]), lambda: moe.Params([a], [g], bits=16),
+                lambda: moe.Params([a], [g], [(codes, scales[:1])], [(z(200, torch.uint8), z(2, torch.uint8))]),
+                lambda: moe.Params([a], [g], [z(200)], [(codes, scales)]),
+                lambda: moe.Params(None, [g], bits=8),
+                # what is written lies apart
+                lambda: moe.Params([a, a], [g, g]), lambda: moe.Params([a], [a]),
+                lambda: moe.Params([a[:150], a[100:200]], [g[:150], g[:100]]),
+                lambda: moe.Params([a], [g], [z(200)], [a])):
+        with pytest.raises(ValueError):
+            bad()
+    p = moe.Params([a], [g])
+    with pytest.raises(ValueError):
+        p.set_grads([g, g])
+    with pytest.raises(ValueError):
+        p.set_grads([a])
+    with pytest.raises(ValueError):
+        moe.moe_adamw_states(p)
+    with pytest.raises(ValueError):
+        moe.moe_adamw_step(moe.Params(None, [g]), 1e-3, 1)
+    with pytest.raises(ValueError):
+        moe.moe_adamw_step(p, torch.zeros(2, device="cuda"), 1)
+    with pytest.raises(moe.MoEError):
+        moe.moe_adamw_step(p, 1e-3, 0)
+    with pytest.raises(moe.MoEError):
+        moe.moe_adamw_step(p, 1e-3, 1, grad_sumsq=z(1), max_norm=0.0)
+    with pytest.raises(moe.MoEError):
+        moe.moe_adamw_step(p, 1e-3, 1, eps=0.0)
+    # gradients may share memory among themselves
+    moe.Params([z(100), z(100)], [g[:100], g[:100]])
