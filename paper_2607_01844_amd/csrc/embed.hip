@@ -7,7 +7,10 @@
 // registers and written; one that passes a piece's end leaves fp32 partial sums,
 // which are joined in order.  Rows without tokens are written as zeros by
 // workgroups that look them up in the sorted list.  Both directions are bound by
-// the HBM stream of their rows, the gradient mostly by writing dW.
+// the HBM stream of their rows, the gradient mostly by writing dW.  65536 tokens,
+// H = 4096: the forward 128 us (5.7 TB/s of rows read and written), sorting 25, sums
+// and zeros of 200,000 rows 405 (5.4 TB/s; 2000 rows: 104), joining 15; with few
+// tokens the launches and their latency (256 tokens, H = 128: 3, then 7, 5 and 3).
 #include <algorithm>
 
 #include "common.h"
@@ -67,7 +70,8 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const int32_t* __restric
 #pragma unroll
         for (int q = 0; q < 8; ++q) f[q] *= scale;
         // an absent row is 0, whatever the scale is
-        if (c0 + u * lanes < nch) dst[c0 + u * lanes] = there ? pack8(f) : make_uint4(0, 0, 0, 0);
+        if (c0 + u * lanes < nch)
+          store_stream(dst + c0 + u * lanes, there ? pack8(f) : make_uint4(0, 0, 0, 0));
       }
     }
   }
@@ -262,22 +266,48 @@ __global__ __launch_bounds__(64 * SORT_W) void embed_place_kernel(
 }
 
 // ---------------------------------------------------------------- gradient
+// The first place with a key of r or more: a whole wave looks, 64 places a step.
+__device__ __forceinline__ int64_t first_not_below(const uint32_t* __restrict__ key, int64_t n,
+                                                   int64_t r) {
+  const int lane = lane_id();
+  int64_t lo = 0;
+  while (n > 0) {
+    const int64_t step = (n + 63) >> 6;
+    const int64_t probe = lo + min((lane + 1) * step, n) - 1;
+    const int below = __popcll(__ballot(key[probe] < r));
+    if (below == 64) return lo + n;
+    lo += below * step;
+    n = min(step, n - below * step) - 1;  // the probe itself is not below
+  }
+  return lo;
+}
+
 // A team of 2^s lanes sums the rows of dy of one piece's tokens over 8 * 2^s
 // columns (a slab).  part [pieces][2][H]: sums of the run that comes from the
 // piece before (0) and of the run that goes on into the next (1).
 // Workgroups from `sums` on write the zeros of rows without tokens.
+// WAVE: a team is a wave (s = 6), and keys and tokens are scalars of it.
+template <bool WAVE>
 __global__ __launch_bounds__(256) void embed_sum_kernel(
     const uint32_t* __restrict__ key, const int32_t* __restrict__ tok,
     const uint16_t* __restrict__ dy, int64_t N, int H, int64_t rows, float scale, int s, int slabs,
     int piece, int64_t sums, float* __restrict__ part, uint16_t* __restrict__ dw) {
-  const int nch = H >> 3, lanes = 1 << s, l = threadIdx.x & (lanes - 1);
-  const int team = threadIdx.x >> s, teams = 256 >> s;
+  const int nch = H >> 3, lanes = WAVE ? 64 : 1 << s, l = threadIdx.x & (lanes - 1);
+  const int team = WAVE ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x >> s;
+  const int teams = WAVE ? 4 : 256 >> s;
   if (blockIdx.x >= sums) {
+    __shared__ int64_t ends[2];
     __shared__ int there[ZERO_ROWS];
     const int64_t row0 = (blockIdx.x - sums) * ZERO_ROWS;
+    // the tokens of these rows lie between two places; each row looks between them
+    if (threadIdx.x < 128) {
+      const int64_t at = first_not_below(key, N, row0 + (threadIdx.x < 64 ? 0 : ZERO_ROWS));
+      if ((threadIdx.x & 63) == 0) ends[threadIdx.x >> 6] = at;
+    }
+    __syncthreads();
     if (threadIdx.x < ZERO_ROWS) {
       const int64_t r = row0 + threadIdx.x;
-      int64_t lo = 0, n = N;  // the first place with a key of r or more
+      int64_t lo = ends[0], n = ends[1] - lo;
       while (n > 0) {
         const int64_t half = n >> 1;
         if (key[lo + half] < r) {
@@ -287,7 +317,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(
           n = half;
         }
       }
-      there[threadIdx.x] = r >= rows || (lo < N && key[lo] == r);
+      there[threadIdx.x] = r >= rows || (lo < ends[1] && key[lo] == r);
     }
     __syncthreads();
     for (int i = team; i < ZERO_ROWS; i += teams) {
@@ -300,14 +330,31 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(
   const int64_t id = static_cast<int64_t>(blockIdx.x) * teams + team;
   const int64_t pc = id / slabs;
   const int c = static_cast<int>(id - pc * slabs) * lanes + l;
-  const int64_t p0 = pc * piece, p1 = min(N, p0 + piece);
-  if (p0 >= N || c >= nch) return;
-  uint32_t cur = key[p0];
+  const int64_t p0 = pc * piece;
+  if (p0 >= N || (!WAVE && c >= nch)) return;
+  const int n = static_cast<int>(min<int64_t>(N - p0, piece));
+  // what lies beyond the row's end is read from its first column, and not written
+  const uint4* col = reinterpret_cast<const uint4*>(dy) + (c < nch ? c : 0);
+  uint32_t kl = 0;
+  int tl = 0;
+  if constexpr (WAVE) {  // a lane a token (pieces are 64 at most)
+    kl = key[p0 + min(l, n - 1)];
+    tl = tok[p0 + min(l, n - 1)];
+  }
+  auto key_at = [&](int i) -> uint32_t {
+    if constexpr (WAVE) return __builtin_amdgcn_readlane(kl, i);
+    else return key[p0 + min(i, n - 1)];
+  };
+  auto tok_at = [&](int i) -> int {
+    if constexpr (WAVE) return __builtin_amdgcn_readlane(tl, i);
+    else return tok[p0 + min(i, n - 1)];
+  };
+  uint32_t cur = key_at(0);
   if (cur >= rows) return;
   bool head = p0 > 0 && key[p0 - 1] == cur;
   float acc[8] = {};
   auto flush = [&](bool tail) {
-    if (cur >= rows) return;
+    if (cur >= rows || (WAVE && c >= nch)) return;
     if (!head && !tail) {
       float f[8];
 #pragma unroll
@@ -319,40 +366,54 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(
       o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
     }
   };
-  constexpr int U = 8;
-  for (int64_t p = p0; p < p1; p += U) {
-    uint32_t k[U];
-    uint4 v[U];
+  // U rows on their way while U are summed (keys and rows asked for one by one, with
+  // a test before each, made 104 us 170); those past the list's end repeat its last
+  // one without being summed.  U = 8 is no faster on whole waves, and on narrow rows,
+  // where it takes 130 registers, slower (20 us: 37)
+  constexpr int U = 4;
+  uint32_t k[2][U];
+  uint4 v[2][U];
+  auto fetch = [&](int i, int b) {
+    int t[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      k[u] = p + u < p1 ? key[p + u] : static_cast<uint32_t>(rows);
-      if (k[u] < rows)
-        v[u] = reinterpret_cast<const uint4*>(dy + static_cast<int64_t>(tok[p + u]) * H)[c];
+      k[b][u] = key_at(i + u);
+      t[u] = tok_at(i + u);
     }
 #pragma unroll
+    for (int u = 0; u < U; ++u)
+      v[b][u] = load_stream(col + static_cast<int64_t>(t[u]) * nch);
+  };
+  auto add = [&](int i, int b) {
+#pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (p + u < p1) {
-        if (k[u] != cur) {
+      if (i + u < n) {
+        if (k[b][u] != cur) {
           flush(false);
-          cur = k[u];
+          cur = k[b][u];
           head = false;
 #pragma unroll
           for (int q = 0; q < 8; ++q) acc[q] = 0.0f;
         }
-        if (k[u] < rows) {
-          float f[8];
-          unpack8(v[u], f);
+        float f[8];
+        unpack8(v[b][u], f);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) acc[q] += f[q];
-        }
+        for (int q = 0; q < 8; ++q) acc[q] += f[q];
       }
     }
+  };
+  fetch(0, 0);
+  for (int i = 0; i < n; i += 2 * U) {
+    if (i + U < n) fetch(i + U, 1);
+    add(i, 0);
+    if (i + 2 * U < n) fetch(i + 2 * U, 0);
+    if (i + U < n) add(i + U, 1);
   }
-  flush(p1 < N && key[p1] == cur);
+  flush(p0 + n < N && key[p0 + n] == cur);
 }
 
-// The runs that pass the end of the piece they begin in: one workgroup a piece
-// and slab; its teams take every teams-th of the run's pieces.
+// The runs that pass the end of the piece they begin in: one workgroup a piece and
+// slab; its teams take every teams-th of the run's pieces, eight loads at a time.
 __global__ __launch_bounds__(256) void embed_join_kernel(
     const uint32_t* __restrict__ key, int64_t N, int H, int64_t rows, float scale, int s, int slabs,
     int piece, const float* __restrict__ part, uint16_t* __restrict__ dw) {
@@ -363,31 +424,49 @@ __global__ __launch_bounds__(256) void embed_join_kernel(
   const int c = static_cast<int>(blockIdx.x - pc * slabs) * lanes + l;
   const int64_t p0 = pc * piece, p1 = p0 + piece;
   if (p1 >= N) return;
-  const uint32_t k = key[p1];
-  if (k >= rows || key[p1 - 1] != k) return;
-  if (key[p0] == k && p0 > 0 && key[p0 - 1] == k) return;  // it began before
-  int64_t more = 0;  // pieces after this one that begin in the run
-  for (;;) {
-    const int64_t at = (pc + 1 + more + (threadIdx.x & 63)) * piece;
-    const uint64_t m = __ballot(at < N && key[at < N ? at : 0] == k);
+  // all at once, for the many that end here
+  const int64_t at0 = (pc + 1 + (threadIdx.x & 63)) * piece;
+  const uint32_t k = key[p1], end = key[p1 - 1], first = key[p0], earlier = key[p0 > 0 ? p0 - 1 : 0];
+  const uint32_t probe = key[at0 < N ? at0 : 0];
+  if (k >= rows || end != k) return;
+  if (first == k && p0 > 0 && earlier == k) return;  // it began before
+  // pieces after this one that begin in the run
+  uint64_t m = __ballot(at0 < N && probe == k);
+  int64_t more = __popcll(m);
+  while (m == ~0ull) {
+    const int64_t at = at0 + more * piece;
+    m = __ballot(at < N && key[at < N ? at : 0] == k);
     more += __popcll(m);
-    if (m != ~0ull) break;
   }
   float acc[8] = {};
   if (c < nch) {
-    for (int64_t i = team; i <= more; i += teams) {
-      const float4* o = reinterpret_cast<const float4*>(
-          part + ((pc + i) * 2 + (i == 0 ? 1 : 0)) * H + 8 * c);
-      const float4 a = o[0], b = o[1];
-      acc[0] += a.x; acc[1] += a.y; acc[2] += a.z; acc[3] += a.w;
-      acc[4] += b.x; acc[5] += b.y; acc[6] += b.z; acc[7] += b.w;
+    constexpr int B = 8;
+    for (int64_t i0 = team; i0 <= more; i0 += B * teams) {
+      float4 a[B], b[B];
+#pragma unroll
+      for (int u = 0; u < B; ++u) {
+        const int64_t i = i0 + u * teams;
+        a[u] = b[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (i <= more) {
+          const float4* o = reinterpret_cast<const float4*>(
+              part + ((pc + i) * 2 + (i == 0 ? 1 : 0)) * H + 8 * c);
+          a[u] = o[0];
+          b[u] = o[1];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < B; ++u) {
+        acc[0] += a[u].x; acc[1] += a[u].y; acc[2] += a[u].z; acc[3] += a[u].w;
+        acc[4] += b[u].x; acc[5] += b[u].y; acc[6] += b[u].z; acc[7] += b[u].w;
+      }
     }
   }
 #pragma unroll
   for (int q = 0; q < 8; ++q) sums[threadIdx.x * 8 + q] = acc[q];
   __syncthreads();
   if (team == 0 && c < nch) {
-    for (int u = 1; u < teams; ++u)
+    const int some = static_cast<int>(min<int64_t>(teams, more + 1));
+    for (int u = 1; u < some; ++u)
 #pragma unroll
       for (int q = 0; q < 8; ++q) acc[q] += sums[(u * lanes + l) * 8 + q];
     float f[8];
@@ -502,10 +581,16 @@ hipError_t launch_embed_bwd(const int32_t* ids, const uint16_t* dy, int64_t N, i
   float* part = reinterpret_cast<float*>(at + p.part);
   const int64_t sums = ceil_div(p.pieces * p.slabs << p.s, 256);
   prof_begin(K_EMBED_SUM, s);
-  embed_sum_kernel<<<static_cast<unsigned>(sums + ceil_div(rows, ZERO_ROWS)), 256, 0, s>>>(
-      key(last), tok(last), dy, N, H, rows, scale, p.s, p.slabs, p.piece, sums, part, dw);
-  embed_join_kernel<<<static_cast<unsigned>(p.pieces * p.slabs), 256, 0, s>>>(
-      key(last), N, H, rows, scale, p.s, p.slabs, p.piece, part, dw);
+  const unsigned grid = static_cast<unsigned>(sums + ceil_div(rows, ZERO_ROWS));
+  if (p.s == 6)
+    embed_sum_kernel<true><<<grid, 256, 0, s>>>(key(last), tok(last), dy, N, H, rows, scale, p.s,
+                                                p.slabs, p.piece, sums, part, dw);
+  else
+    embed_sum_kernel<false><<<grid, 256, 0, s>>>(key(last), tok(last), dy, N, H, rows, scale, p.s,
+                                                 p.slabs, p.piece, sums, part, dw);
+  if (p.pieces > 1)
+    embed_join_kernel<<<static_cast<unsigned>((p.pieces - 1) * p.slabs), 256, 0, s>>>(
+        key(last), N, H, rows, scale, p.s, p.slabs, p.piece, part, dw);
   prof_end(K_EMBED_SUM, s);
   return hipGetLastError();
 }
