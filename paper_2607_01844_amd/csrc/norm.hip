@@ -6,7 +6,9 @@
 // A row is held in registers by W waves, so each operand crosses HBM once; the
 // mean is subtracted before the squares are summed (a row far from zero keeps its
 // variance).  Sums, statistics and the weights' gradients are fp32; every
-// bf16 result is rounded once.  Bound by the HBM stream.
+// bf16 result is rounded once.  Bound by the HBM stream: T = 65536, d = 4096 with the
+// residual, 2.1 GB each way, forward 5.7 to 6 TB/s, backward 5.7 to 6.2; few rows by
+// latency (16 of them: 4 us).
 #include <algorithm>
 
 #include "common.h"
@@ -38,6 +40,12 @@ __device__ __forceinline__ void load8f(const float* __restrict__ p, float* f) {
   f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
 
+template <bool STREAM>
+__device__ __forceinline__ uint4 load_row(const uint4* p) {
+  if constexpr (STREAM) return load_stream(p);
+  else return *p;
+}
+
 // Over the W waves of a row: the sums of n values, in every lane.  `red` is this
 // exchange's own place; with two exchanges a round, one barrier each is enough.
 template <int W, int N>
@@ -58,15 +66,16 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* red, int w, int l
   }
 }
 
-// Waves of a row W, chunks of 8 columns a lane C, rows at once R.  Chunk c of
-// lane l of wave w: (c W + w) 64 + l.
-template <int W, int C, int R, bool RES>
+// Waves of a row W, chunks of 8 columns a lane C; chunk c of lane l of wave w is
+// (c W + w) 64 + l.  STREAM: loads that no cache keeps.
+template <int W, int C, bool RES, bool STREAM>
 __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_fwd_kernel(
     const uint16_t* __restrict__ x, const uint16_t* __restrict__ res,
     const float* __restrict__ gamma, const float* __restrict__ beta, int64_t T, int d, float eps,
     uint16_t* __restrict__ h, uint16_t* __restrict__ y, float* __restrict__ mean,
     float* __restrict__ rstd) {
   constexpr int G = W < 4 ? 4 / W : 1;  // rows' teams of a workgroup
+  constexpr int R = 1;                  // rows at once (2: no faster)
   __shared__ float red[2][R * W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int w = wave % W, team = wave / W;
@@ -93,8 +102,8 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_fwd_kernel(
         const int at = (c * W + w) * 64 + lane;
         v[r][c] = make_uint4(0, 0, 0, 0);
         if (at < nch && t0 + r < T) {
-          v[r][c] = reinterpret_cast<const uint4*>(x + (t0 + r) * d)[at];
-          if constexpr (RES) e[r][c] = reinterpret_cast<const uint4*>(res + (t0 + r) * d)[at];
+          v[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(x + (t0 + r) * d) + at);
+          if constexpr (RES) e[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(res + (t0 + r) * d) + at);
         }
       }
     if constexpr (RES) {
@@ -105,7 +114,7 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_fwd_kernel(
           const int at = (c * W + w) * 64 + lane;
           if (at < nch && t0 + r < T) {
             v[r][c] = add8(v[r][c], e[r][c]);
-            reinterpret_cast<uint4*>(h + (t0 + r) * d)[at] = v[r][c];
+            store_stream(reinterpret_cast<uint4*>(h + (t0 + r) * d) + at, v[r][c]);
           }
         }
     }
@@ -147,7 +156,7 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_fwd_kernel(
           unpack8(v[r][c], f);
 #pragma unroll
           for (int q = 0; q < 8; ++q) f[q] = (f[q] - mu[r]) * rs * ga[c][q] + be[c][q];
-          if (at < nch) reinterpret_cast<uint4*>(y + (t0 + r) * d)[at] = pack8(f);
+          if (at < nch) store_stream(reinterpret_cast<uint4*>(y + (t0 + r) * d) + at, pack8(f));
         }
         if (w == 0 && lane == 0) {
           if (mean) mean[t0 + r] = mu[r];
@@ -159,13 +168,13 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_fwd_kernel(
 }
 
 // part [workgroups][2][d]: the workgroup's sums of dy xh and of dy.
-template <int W, int C, int R, bool DH>
+template <int W, int C, bool DH, bool STREAM>
 __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_bwd_kernel(
     const uint16_t* __restrict__ dy, const uint16_t* __restrict__ h,
     const float* __restrict__ gamma, const float* __restrict__ mean,
     const float* __restrict__ rstd, const uint16_t* __restrict__ dh, int64_t T, int d,
     uint16_t* __restrict__ dx, float* __restrict__ part) {
-  constexpr int G = W < 4 ? 4 / W : 1;
+  constexpr int G = W < 4 ? 4 / W : 1, R = 1;
   __shared__ float red[2][2 * R * W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int w = wave % W, team = wave / W;
@@ -194,9 +203,9 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_bwd_kernel(
         const int at = (c * W + w) * 64 + lane;
         a[r][c] = b[r][c] = make_uint4(0, 0, 0, 0);
         if (at < nch && in) {
-          a[r][c] = reinterpret_cast<const uint4*>(dy + (t0 + r) * d)[at];
-          b[r][c] = reinterpret_cast<const uint4*>(h + (t0 + r) * d)[at];
-          if constexpr (DH) e[r][c] = reinterpret_cast<const uint4*>(dh + (t0 + r) * d)[at];
+          a[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(dy + (t0 + r) * d) + at);
+          b[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(h + (t0 + r) * d) + at);
+          if constexpr (DH) e[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(dh + (t0 + r) * d) + at);
         }
       }
     }
@@ -245,7 +254,11 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_bwd_kernel(
 #pragma unroll
             for (int q = 0; q < 8; ++q) f[q] += g[q];
           }
-          if (at < nch) reinterpret_cast<uint4*>(dx + (t0 + r) * d)[at] = pack8(f);
+          if (at < nch) {
+            uint4* o = reinterpret_cast<uint4*>(dx + (t0 + r) * d) + at;
+            if constexpr (STREAM) store_stream(o, pack8(f));
+            else *o = pack8(f);
+          }
         }
       }
     }
@@ -409,30 +422,33 @@ __global__ __launch_bounds__(256) void norm_cols_kernel(
   }
 }
 
-// out[i] = sum over parts of part[p][i]: 64 columns a workgroup, its 4 waves take
-// every fourth part (joined in order), dgamma then dbeta (null: not wanted).
-__global__ __launch_bounds__(256) void norm_sum_kernel(const float* __restrict__ part, int parts,
-                                                       int d, float* __restrict__ dgamma,
-                                                       float* __restrict__ dbeta) {
-  __shared__ float sums[4][64];
+// out[i] = sum over parts of part[p][i]: 64 columns a workgroup, its 16 waves take
+// every 16th part (joined in order), dgamma then dbeta (null: not wanted).
+constexpr int SUM_W = 16;
+__global__ __launch_bounds__(64 * SUM_W) void norm_sum_kernel(const float* __restrict__ part,
+                                                              int parts, int d,
+                                                              float* __restrict__ dgamma,
+                                                              float* __restrict__ dbeta) {
+  __shared__ float sums[SUM_W][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 64 + lane, pitch = 2 * static_cast<int64_t>(d);
+  constexpr int B = 8;
   float s = 0.0f;
-  if (i < 2 * d) {
+  if (i < pitch) {
     int p = w;
-    for (; p + 28 < parts; p += 32) {
-      float v[8];
+    for (; p + (B - 1) * SUM_W < parts; p += B * SUM_W) {
+      float v[B];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = part[static_cast<int64_t>(p + 4 * u) * 2 * d + i];
+      for (int u = 0; u < B; ++u) v[u] = part[(p + u * SUM_W) * pitch + i];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) s += v[u];
+      for (int u = 0; u < B; ++u) s += v[u];
     }
-    for (; p < parts; p += 4) s += part[static_cast<int64_t>(p) * 2 * d + i];
+    for (; p < parts; p += SUM_W) s += part[p * pitch + i];
   }
   sums[w][lane] = s;
   __syncthreads();
-  if (w == 0 && i < 2 * d) {
-    s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+  if (w == 0 && i < pitch) {
+    for (int u = 1; u < SUM_W; ++u) s += sums[u][lane];
     if (i < d)
       dgamma[i] = s;
     else if (dbeta)
@@ -442,23 +458,45 @@ __global__ __launch_bounds__(256) void norm_sum_kernel(const float* __restrict__
 
 constexpr int NORM_HELD = 16384;  // widest row held in registers
 
-// Workgroups of a backward pass: what is resident, less where each would have
-// few rows (their partial sums, 8 bytes a column, weigh against 6 a row's).
+// Two workgroups a compute unit walk the rows (three of narrow rows, one of 16 waves in
+// the backward pass): few rows in flight, far apart, suit HBM best (T = 65536, d = 4096,
+// 2.1 GB each way: forward 358 us on 512 workgroups, 379 on 768, 398 on 2048; backward
+// 342, 373, 394; d = 512: 39, 38 and 45, 43).
+// A backward pass has fewer where a team would get under 16 rows: its partial sums,
+// 8 bytes a column, weigh against 6 or 8 a row's (T = 4096, d = 8192: 64 us on 256
+// workgroups, 67 on 512, 90 on 1024).
+int64_t groups_a_cu(int d) { return d <= 1024 ? 3 : 2; }
 int64_t bwd_groups(int64_t T, int d) {
+  if (T == 0) return 1;
   if (d > NORM_HELD) return std::clamp<int64_t>(T / 64, 1, 64);
-  const int64_t teams = d <= 1024 ? 4 : 1;
-  return std::clamp<int64_t>(ceil_div(T, 4 * teams), 1, d <= 4096 ? 768 : d <= 8192 ? 512 : 256);
+  const int64_t teams = d <= 2048 ? 4 : 1, most = d <= 8192 ? 256 * groups_a_cu(d) : 256;
+  const int64_t rows = std::max(ceil_div(T, teams * most),
+                                std::min<int64_t>(16, ceil_div(T, teams * 256)));  // of a team
+  return std::max<int64_t>(1, ceil_div(T, teams * rows));
 }
 
+// Calls that move this much gain from keeping their reads out of the caches (and the
+// backward's dx): forward of 2.1 GB 366 -> 358 us, backward 385 -> 342, of 470 MB
+// 104 -> 94; less may find its inputs there (forward of 268 MB 40 us, with streamed
+// loads 47; backward 48 and 49).  y and h are streamed always (268 MB: 44 -> 37 us).
+constexpr int64_t STREAM_FWD = int64_t{768} << 20, STREAM_BWD = int64_t{384} << 20;
+
+// A wave a row up to 2048 columns (32 registers of it a lane), then eight and sixteen.
 template <typename F>
 void by_width(int d, F&& f) {
   using std::integral_constant;
   if (d <= 512) f(integral_constant<int, 1>{}, integral_constant<int, 1>{});
   else if (d <= 1024) f(integral_constant<int, 1>{}, integral_constant<int, 2>{});
-  else if (d <= 2048) f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-  else if (d <= 4096) f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-  else if (d <= 8192) f(integral_constant<int, 4>{}, integral_constant<int, 4>{});
-  else f(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+  else if (d <= 2048) f(integral_constant<int, 1>{}, integral_constant<int, 4>{});
+  else if (d <= 4096) f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+  else if (d <= 8192) f(integral_constant<int, 8>{}, integral_constant<int, 2>{});
+  else f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+}
+// f(true_type) or f(false_type)
+template <typename F>
+void either(bool v, F&& f) {
+  if (v) f(std::true_type{});
+  else f(std::false_type{});
 }
 
 }  // namespace
@@ -475,13 +513,20 @@ hipError_t launch_norm_fwd(const uint16_t* x, const uint16_t* res, const float* 
     else
       norm_fwd_long_kernel<false><<<grid, 1024, 0, s>>>(x, res, gamma, beta, T, d, eps, h, y, mean, rstd);
   } else {
+    const bool stream = T * d * (res ? 8 : 4) >= STREAM_FWD;
     by_width(d, [&](auto w, auto c) {
       constexpr int W = w, C = c, G = W < 4 ? 4 / W : 1, threads = W < 4 ? 256 : 64 * W;
-      const unsigned grid = static_cast<unsigned>(std::min<int64_t>(ceil_div(T, G), 8 * device_cus()));
-      if (res)
-        norm_fwd_kernel<W, C, 1, true><<<grid, threads, 0, s>>>(x, res, gamma, beta, T, d, eps, h, y, mean, rstd);
-      else
-        norm_fwd_kernel<W, C, 1, false><<<grid, threads, 0, s>>>(x, res, gamma, beta, T, d, eps, h, y, mean, rstd);
+      // one load of 16 bytes a lane and row is too little in flight (T = 65536, d = 4096
+      // without the residual: 226 us, with twice the workgroups 196)
+      const int more = !res && W > 1 && C == 1 ? 2 : 1;
+      const unsigned grid = static_cast<unsigned>(
+          std::min<int64_t>(ceil_div(T, G), more * groups_a_cu(d) * device_cus()));
+      either(res != nullptr, [&](auto r) {
+        either(stream, [&](auto st) {
+          norm_fwd_kernel<W, C, r, st><<<grid, threads, 0, s>>>(x, res, gamma, beta, T, d, eps, h,
+                                                                y, mean, rstd);
+        });
+      });
     });
   }
   prof_end(K_NORM_FWD, s);
@@ -509,19 +554,21 @@ hipError_t launch_norm_bwd(const uint16_t* dy, const uint16_t* h, const float* g
       const dim3 cols(static_cast<unsigned>(ceil_div(d, 2048)), static_cast<unsigned>(groups));
       norm_cols_kernel<<<cols, 256, 0, s>>>(dy, h, mean, rstd, T, d, ceil_div(T, groups), part);
     } else {
+      const bool stream = T * d * (dh ? 8 : 6) >= STREAM_BWD;
       by_width(d, [&](auto w, auto c) {
         constexpr int W = w, C = c, threads = W < 4 ? 256 : 64 * W;
-        const unsigned grid = static_cast<unsigned>(groups);
-        if (dh)
-          norm_bwd_kernel<W, C, 1, true><<<grid, threads, 0, s>>>(dy, h, gamma, mean, rstd, dh, T, d, dx, part);
-        else
-          norm_bwd_kernel<W, C, 1, false><<<grid, threads, 0, s>>>(dy, h, gamma, mean, rstd, dh, T, d, dx, part);
+        either(dh != nullptr, [&](auto r) {
+          either(stream, [&](auto st) {
+            norm_bwd_kernel<W, C, r, st><<<static_cast<unsigned>(groups), threads, 0, s>>>(
+                dy, h, gamma, mean, rstd, dh, T, d, dx, part);
+          });
+        });
       });
     }
     prof_end(K_NORM_BWD, s);
   }
   prof_begin(K_NORM_SUM, s);
-  norm_sum_kernel<<<static_cast<unsigned>(ceil_div(2 * static_cast<int64_t>(d), 64)), 256, 0, s>>>(
+  norm_sum_kernel<<<static_cast<unsigned>(ceil_div(2 * static_cast<int64_t>(d), 64)), 64 * SUM_W, 0, s>>>(
       part, static_cast<int>(groups), d, dgamma, dbeta);
   prof_end(K_NORM_SUM, s);
   return hipGetLastError();
