@@ -40,7 +40,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 
 
 def _stream():
-    return _raw_stream(torch.cuda.current_device())
+    # (callers hold device tensors: the runtime is up, and its own call is enough)
+    return _raw_stream(torch._C._cuda_getDevice())
 
 
 @functools.lru_cache(maxsize=512, typed=True)
@@ -651,31 +652,46 @@ def moe_vocab_distill_bwd(x, w_voc, topk_idx, topk_logit, lse, y_topk, dloss, vb
 
 
 # --------------------------------------------------------------- embedding
+def _given_2d(t, name):
+    """(rows, columns) of a bf16 matrix on the current device."""
+    if (t is not None and t.dtype is torch.bfloat16 and t.is_cuda and t.dim() == 2 and
+            t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice()):
+        return t.shape
+    _need(t, torch.bfloat16, name, 2)
+    return _given(t, torch.bfloat16, name, t.shape).shape
+
+
+def _like(t, like, name):
+    """An output of the shape and type of `like`: the caller's, checked, or new."""
+    if t is None:
+        return torch.empty_like(like)
+    return _given(t, like.dtype, name, like.shape)
+
+
 def moe_embedding_fwd(ids, w, scale=1.0, vocab_begin=0, y=None):
     """Rows of w [rows,H] bf16 (vocabulary entries [vocab_begin, vocab_begin +
     rows)) for ids [N] int32, times scale; zeros for ids outside them (another
     rank's, or -1 for padding).  Returns y [N,H] bf16."""
-    _need(w, torch.bfloat16, "w", 2)
+    rows, H = _given_2d(w, "w")
     _need(ids, torch.int32, "ids", 1)
-    rows, H = _given(w, torch.bfloat16, "w", w.shape).shape
     N = _given(ids, torch.int32, "ids", ids.shape).shape[0]
-    y = _out(y, torch.bfloat16, "y", (N, H), w.device)
-    _check(lib.moe_embedding_fwd(_ptr(ids), _ptr(w), N, H, vocab_begin, rows, scale, _ptr(y),
-                                 _stream()), "moe_embedding_fwd")
+    y = w.new_empty((N, H)) if y is None else _given(y, torch.bfloat16, "y", (N, H))
+    _check(lib.moe_embedding_fwd(ids.data_ptr(), w.data_ptr(), N, H, vocab_begin, rows, scale,
+                                 y.data_ptr(), _stream()), "moe_embedding_fwd")
     return y
 
 
 def moe_embedding_bwd(ids, dy, rows, scale=1.0, vocab_begin=0, dw=None):
     """Gradient of the embedding's weights from dy [N,H] bf16: dw [rows,H] bf16,
     every row written (zeros where no token named it)."""
-    _need(dy, torch.bfloat16, "dy", 2)
-    N, H = _given(dy, torch.bfloat16, "dy", dy.shape).shape
+    N, H = _given_2d(dy, "dy")
     _given(ids, torch.int32, "ids", (N,))
     ws = workspace(_ws_bytes("moe_embedding_bwd_workspace_bytes", N, H, rows), dy.device,
                    "embedding_bwd")
-    dw = _out(dw, torch.bfloat16, "dw", (rows, H), dy.device)
-    _check(lib.moe_embedding_bwd(_ptr(ids), _ptr(dy), N, H, vocab_begin, rows, scale, _ptr(dw),
-                                 _ptr(ws), ws.numel(), _stream()), "moe_embedding_bwd")
+    dw = dy.new_empty((rows, H)) if dw is None else _given(dw, torch.bfloat16, "dw", (rows, H))
+    _check(lib.moe_embedding_bwd(ids.data_ptr(), dy.data_ptr(), N, H, vocab_begin, rows, scale,
+                                 dw.data_ptr(), ws.data_ptr(), ws.numel(), _stream()),
+           "moe_embedding_bwd")
     return dw
 
 
@@ -684,22 +700,21 @@ def moe_layer_norm_fwd(x, gamma, beta=None, eps=1e-5, residual=None, y=None, h=N
     """Layer norm of h = x + residual (rounded to bf16; h is x without a
     residual), rows [T,d] bf16, gamma and beta [d] fp32.  Returns (y, h, mean
     [T], rstd [T]); stats=False: None in the place of the last two."""
-    _need(x, torch.bfloat16, "x", 2)
-    T, d = _given(x, torch.bfloat16, "x", x.shape).shape
+    T, d = shape = _given_2d(x, "x")
     _given(gamma, torch.float32, "gamma", (d,))
     if beta is not None:
         _given(beta, torch.float32, "beta", (d,))
-    dev = x.device
     if residual is not None:
-        _given(residual, torch.bfloat16, "residual", (T, d))
-        h = _out(h, torch.bfloat16, "h", (T, d), dev)
+        _given(residual, torch.bfloat16, "residual", shape)
+        h = _like(h, x, "h")
     elif h is not None:
         raise ValueError("h is an output of a residual sum: without residual it is x")
-    y = _out(y, torch.bfloat16, "y", (T, d), dev)
-    mean = torch.empty((T,), dtype=torch.float32, device=dev) if stats else None
-    rstd = torch.empty((T,), dtype=torch.float32, device=dev) if stats else None
-    _check(lib.moe_layer_norm_fwd(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), T, d, eps,
-                                  _ptr(h), _ptr(y), _ptr(mean), _ptr(rstd), _stream()),
+    y = _like(y, x, "y")
+    mean = rstd = None
+    if stats:
+        mean, rstd = gamma.new_empty((T,)), gamma.new_empty((T,))
+    _check(lib.moe_layer_norm_fwd(x.data_ptr(), _ptr(residual), gamma.data_ptr(), _ptr(beta), T, d,
+                                  eps, _ptr(h), y.data_ptr(), _ptr(mean), _ptr(rstd), _stream()),
            "moe_layer_norm_fwd")
     return y, x if residual is None else h, mean, rstd
 
@@ -709,21 +724,20 @@ def moe_layer_norm_bwd(dy, h, gamma, mean, rstd, dh=None, dx=None, with_dbeta=Tr
     rstd; dh [T,d]: the gradient that reaches h by another way (the residual
     stream's), added to dx.  Returns (dx [T,d] bf16, dgamma [d], dbeta [d] or
     None, fp32); dx is the gradient of x and of the residual alike."""
-    _need(h, torch.bfloat16, "h", 2)
-    T, d = _given(h, torch.bfloat16, "h", h.shape).shape
-    _given(dy, torch.bfloat16, "dy", (T, d))
+    T, d = shape = _given_2d(h, "h")
+    _given(dy, torch.bfloat16, "dy", shape)
     _given(gamma, torch.float32, "gamma", (d,))
     _given(mean, torch.float32, "mean", (T,))
     _given(rstd, torch.float32, "rstd", (T,))
     if dh is not None:
-        _given(dh, torch.bfloat16, "dh", (T, d))
-    dev = h.device
-    ws = workspace(_ws_bytes("moe_layer_norm_bwd_workspace_bytes", T, d), dev, "layer_norm_bwd")
-    dx = _out(dx, torch.bfloat16, "dx", (T, d), dev)
-    dgamma = torch.empty((d,), dtype=torch.float32, device=dev)
-    dbeta = torch.empty((d,), dtype=torch.float32, device=dev) if with_dbeta else None
-    _check(lib.moe_layer_norm_bwd(_ptr(dy), _ptr(h), _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dh),
-                                  T, d, _ptr(dx), _ptr(dgamma), _ptr(dbeta), _ptr(ws), ws.numel(),
+        _given(dh, torch.bfloat16, "dh", shape)
+    ws = workspace(_ws_bytes("moe_layer_norm_bwd_workspace_bytes", T, d), h.device, "layer_norm_bwd")
+    dx = _like(dx, h, "dx")
+    dgamma = torch.empty_like(gamma)
+    dbeta = torch.empty_like(gamma) if with_dbeta else None
+    _check(lib.moe_layer_norm_bwd(dy.data_ptr(), h.data_ptr(), gamma.data_ptr(), mean.data_ptr(),
+                                  rstd.data_ptr(), _ptr(dh), T, d, dx.data_ptr(),
+                                  dgamma.data_ptr(), _ptr(dbeta), ws.data_ptr(), ws.numel(),
                                   _stream()), "moe_layer_norm_bwd")
     return dx, dgamma, dbeta
 
@@ -747,7 +761,7 @@ class Params:
     def __init__(self, w, g, m=None, v=None, w_copy=None, bits=None):
         self.g = list(g)
         self.count = count = len(self.g)
-        self.device = None
+        self.device = self.torch_device = None
         self.array = (Param * max(count, 1))()
         self.w = None if w is None else list(w)
         self.w_copy = [None] * count if w_copy is None else list(w_copy)
@@ -831,7 +845,7 @@ class Params:
         if t.numel() != n:
             raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
         if self.device is None:
-            self.device = t.get_device()
+            self.device, self.torch_device = t.get_device(), t.device
         if t.get_device() != self.device:
             raise ValueError(f"{name} is on {t.device}, not on the other tensors' device")
         if n:
@@ -878,8 +892,8 @@ def moe_grad_sumsq(params, sumsq=None):
     if not isinstance(params, Params):
         params = Params(None, params)
     params.on_device()
-    dev = torch._C._cuda_getDevice()
-    sumsq = _out(sumsq, torch.float32, "sumsq", (1,), f"cuda:{dev}")
+    dev = params.torch_device or torch.device("cuda", torch.cuda.current_device())
+    sumsq = _out(sumsq, torch.float32, "sumsq", (1,), dev)
     ws = workspace(params.sumsq_bytes, dev, "grad_sumsq")
     _check(lib.moe_grad_sumsq(params.array, params.count, _ptr(sumsq), _ptr(ws), ws.numel(),
                               _stream()), "moe_grad_sumsq")
@@ -924,7 +938,7 @@ def moe_adamw_states(params, m=None, v=None):
         given = [None] * params.count if given is None else list(given)
         if len(given) != params.count:
             raise ValueError(f"{name} needs one entry for each tensor")
-        out.append([_out(t, torch.float32, f"{name}[{i}]", (n,), f"cuda:{params.device}")
+        out.append([_out(t, torch.float32, f"{name}[{i}]", (n,), params.torch_device)
                     for i, (t, n) in enumerate(zip(given, params.sizes))])
     at = [(ctypes.c_void_p * max(params.count, 1))(*[t.data_ptr() for t in o]) for o in out]
     _check(lib.moe_adamw_states(params.array, params.count, *at, _stream()), "moe_adamw_states")
