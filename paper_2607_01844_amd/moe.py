@@ -1026,8 +1026,23 @@ def layer_fwd_bwd(inp: dict, k: int, expert_begin=0, num_local=None, renorm=0,
     tokens as its peers) dx, dw_router and dbias are this rank's terms of sums
     over the ranks; num_local / E of the two losses' gradient is in each, so
     that the sums hold it once.  balance and zloss are whole on every rank.
+
+    With inp["norm_gamma"] (and, optionally, norm_beta, norm_eps and residual) the
+    layer stands in a pre-norm block: h = x + residual, y is the layer's output on
+    the layer norm of h, and dy the gradient of h + y (the next norm's sum), which
+    reaches h both ways; dx is then the gradient of h, and h, dgamma and dbeta are
+    returned.  All experts have to be local: the ranks' dx would each hold dy.
     """
     x = inp["x"]
+    norm = None
+    if inp.get("norm_gamma") is not None:
+        if num_local not in (None, inp["w_router"].shape[1]):
+            raise ValueError("a block's norm needs all experts on this rank")
+        norm = moe_layer_norm_fwd(x, inp["norm_gamma"], inp.get("norm_beta"),
+                                  inp.get("norm_eps", 1e-5), inp.get("residual"))
+        x = norm[0]
+    elif inp.get("residual") is not None:
+        raise ValueError("residual needs norm_gamma")
     E = inp["w_router"].shape[1]
     num_local = E if num_local is None else num_local
     logits = None
@@ -1058,6 +1073,11 @@ def layer_fwd_bwd(inp: dict, k: int, expert_begin=0, num_local=None, renorm=0,
         out.update(balance=balance, zloss=zloss, expert_counts=counts, dw_router=dwr)
         if dbias is not None:
             out["dbias"] = dbias
+    if norm is not None:
+        _, h, mean, rstd = norm
+        dx, dgamma, dbeta = moe_layer_norm_bwd(dx, h, inp["norm_gamma"], mean, rstd, inp["dy"],
+                                               with_dbeta=inp.get("norm_beta") is not None)
+        out.update(dx=dx, h=h, dgamma=dgamma, dbeta=dbeta)
     if keep:
         out.update(pm)
         out.update(h_gate=hg, h_up=hu, y_perm=y_perm, dy_perm=dy_perm, dx_perm=dx_perm)

@@ -148,6 +148,25 @@ def test_first_steps_from_zero_states(bits):
         t["w"] = [x.cpu() for x in p.w]
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("size", [1e-20, 1e-12, 1e16])
+def test_small_and_large_gradients(bits, size):
+    # v' below the normal numbers of fp32, and near its largest
+    from paper_2607_01844_amd import moe
+    t = make([129, 2500], 12, bits, (F32,), (F32,), history=False)
+    for g in t["g"]:
+        g.clamp_(-3, 3).mul_(size)
+    p = on_gpu(t, moe)
+    h = dict(HYPER, eps=1e-30)
+    moe.moe_adamw_step(p, step=1, seed=4, **h)
+    old = HYPER["eps"]
+    HYPER["eps"] = 1e-30
+    try:
+        check(t, p, bits, 1, None, 1.0, 4)
+    finally:
+        HYPER["eps"] = old
+
+
 def test_many_tensors_in_several_launches():
     from paper_2607_01844_amd import moe
     sizes = [(i * 37) % 300 for i in range(131)] + [0, 0, 5, 0]
