@@ -634,8 +634,9 @@ int moe_grad_sumsq(const moe_param* params, int count, float* sumsq, void* works
  * r * 0xBB67AE85 (not to the nearest, which would lose steps under half of a
  * weight's last bit); the copy of fp32 weights is rounded to the nearest.
  *
- * Limits: bits 8 or 32; 0 <= beta < 1, eps >= 1e-30, max_norm > 0 (infinity: no
- * clipping, but steps are left out as above), n < 2^40, t < 2^31.
+ * Limits: bits 8 or 32; 0 <= beta < 1, eps >= 1e-20 (a gradient whose square is
+ * below fp32's smallest number, 1e-45, is divided by eps alone), max_norm > 0
+ * (infinity: no clipping, but steps are left out as above), n < 2^40, t < 2^31.
  */
 typedef struct moe_adamw_options {
   double lr;

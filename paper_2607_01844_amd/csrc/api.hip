@@ -1010,7 +1010,7 @@ MOE_API int moe_adamw_step(const moe_param* params, int count, int bits,
   CHECK(o.lr_device != nullptr || std::isfinite(o.lr), "lr is not finite");
   CHECK(o.beta1 >= 0.0 && o.beta1 < 1.0, "beta1 out of [0, 1)");
   CHECK(o.beta2 >= 0.0 && o.beta2 < 1.0, "beta2 out of [0, 1)");
-  CHECK(std::isfinite(o.eps) && o.eps >= 1e-30, "eps must be finite and 1e-30 or more");
+  CHECK(std::isfinite(o.eps) && o.eps >= 1e-20, "eps must be finite and 1e-20 or more");
   CHECK(std::isfinite(o.weight_decay), "weight_decay is not finite");
   CHECK(o.step_device != nullptr || (o.step >= 1 && o.step < (int64_t{1} << 31)),
         "step out of [1, 2^31)");

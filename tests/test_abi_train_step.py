@@ -96,7 +96,7 @@ INVALID = [
     ("sumsq misaligned out", sumsq(out=MIS)),
     ("adamw bits", step(bits=16)), ("adamw no options", step(opt=False)), ("adamw count", step(count=-1)),
     ("adamw lr", step(lr=math.nan)), ("adamw beta1", step(beta1=1.0)), ("adamw beta2", step(beta2=-0.1)),
-    ("adamw beta nan", step(beta2=math.nan)), ("adamw eps", step(eps=0.0)),
+    ("adamw beta nan", step(beta2=math.nan)), ("adamw eps", step(eps=0.0)), ("adamw eps small", step(eps=9e-21)),
     ("adamw decay", step(weight_decay=math.inf)), ("adamw step 0", step(step=0)),
     ("adamw step large", step(step=1 << 31)), ("adamw max_norm", step(grad_sumsq=4096, max_norm=0.0)),
     ("adamw max_norm nan", step(grad_sumsq=4096, max_norm=math.nan)),
