@@ -499,9 +499,11 @@ Plan plan_bwd(int64_t N, int H, int64_t rows) {
   Plan p{};
   p.s = team_shift(H);
   p.slabs = static_cast<int>(ceil_div(H, 8 << p.s));
-  // tokens of a piece: enough teams to fill the chip first
+  // tokens of a piece: some 1024 waves come first, longer pieces then (they leave fewer
+  // runs to join: 16384 tokens, half of them one word, H = 2048, over 1000 rows take
+  // 38 us, with 8192 waves of 8 tokens 68; with 256 waves 4096 tokens take 36 for 30)
   p.piece = 8;
-  while (p.piece < 64 && ceil_div(N, 2 * p.piece) * p.slabs << p.s >= 8192 * 64) p.piece *= 2;
+  while (p.piece < 64 && ceil_div(N, 2 * p.piece) * p.slabs << p.s >= 1024 * 64) p.piece *= 2;
   p.pieces = ceil_div(N, p.piece);
   int bits = 1;
   while ((rows >> bits) > 0) ++bits;  // keys 0 .. rows
