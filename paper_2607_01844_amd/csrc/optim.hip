@@ -6,7 +6,7 @@
 // captured one replays with the addresses it was given; a launch's workgroups are
 // dealt out over the pieces of all its tensors, a piece each, neighbours on one XCD.
 // Bound by the HBM stream: 28 bytes an element with fp32 states, weights and a bf16
-// copy (619 M elements: 3.11 ms, 5.6 TB/s), 16 with 8-bit states (1.72 ms, 5.8 TB/s;
+// copy (619 M elements: 3.00 ms, 5.8 TB/s), 16 with 8-bit states (1.71 ms, 5.8 TB/s;
 // a copy of 2 GiB moves 5.6 to 5.9).  Whole pieces take a path of their own: with
 // every access behind its own test the 8-bit step took 1.95 ms.
 //
@@ -27,11 +27,15 @@ namespace moe {
 namespace {
 
 constexpr int MANY = 48;     // tensors of a launch (their table within the argument space)
-constexpr int U = 2;         // groups of four elements a lane
-constexpr int PIECE = 1024 * U;
+// Groups of four elements a lane, 1024 apart: a workgroup's piece is 1024 of them.
+// 619 M elements: 32-bit step 3.00 ms with one, 3.12 with two, 3.16 with four; 8-bit
+// step 1.85, 1.71, 1.72; reading 8-bit states 1.06, 1.14, 1.14.
+template <int BITS>
+constexpr int GROUPS = BITS == 8 ? 2 : 1;
+constexpr int GROUPS_READ = 1;
 constexpr int SUM_PIECE = 16384;
 constexpr int SUM_GRID = 2048;
-constexpr int64_t MAX_GRID = int64_t{1} << 22;
+constexpr int64_t MAX_GRID = int64_t{1} << 23;  // workgroups of a launch, 2^31 lanes
 
 struct Tensors {
   moe_param p[MANY];
@@ -211,6 +215,7 @@ struct StepArgs {
 template <int BITS, bool WHOLE>
 __device__ __forceinline__ void adamw_piece(const moe_param& p, int64_t base, const Step& st,
                                             float clip, uint32_t key) {
+  constexpr int U = GROUPS<BITS>;
   float w[U][4], g[U][4], m[U][4], v[U][4];
   uint32_t mc[U], vc[U], ms[U], vs[U];
   int in[U];
@@ -298,6 +303,7 @@ __device__ __forceinline__ void adamw_piece(const moe_param& p, int64_t base, co
 
 template <int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(const Tensors a, const StepArgs o) {
+  constexpr int PIECE = 1024 * GROUPS<BITS>;
   __shared__ Step shared_step;
   __shared__ uint32_t shared_t;
   const int tid = threadIdx.x;
@@ -342,6 +348,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(const Tensors a, const StepA
 // a launch's table has no other use for.
 template <bool WHOLE>
 __device__ __forceinline__ void states_piece(const moe_param& p, int64_t base) {
+  constexpr int U = GROUPS_READ;
   uint32_t mc[U], vc[U], ms[U], vs[U];
   int in[U];
 #pragma unroll
@@ -367,6 +374,7 @@ __device__ __forceinline__ void states_piece(const moe_param& p, int64_t base) {
   }
 }
 __global__ __launch_bounds__(256) void adamw_states_kernel(const Tensors a) {
+  constexpr int PIECE = 1024 * GROUPS_READ;
   for (int64_t c = first_piece(); c < a.first[a.count]; c += gridDim.x) {
     const int j = tensor_of(a, c);
     const moe_param& p = a.p[j];
@@ -496,7 +504,7 @@ hipError_t launch_adamw(const moe_param* params, int count, int bits, const moe_
   o.lr_dev = opt.lr_device; o.step_dev = opt.step_device; o.sumsq = opt.grad_sumsq;
   o.seed = opt.seed;
   prof_begin(K_ADAMW, s);
-  const bool any = in_launches(params, count, PIECE, [&](const Tensors& a, int first) {
+  const bool any = in_launches(params, count, 1024 * (bits == 32 ? GROUPS<32> : GROUPS<8>), [&](const Tensors& a, int first) {
     o.first_tensor = static_cast<uint32_t>(first);
     const unsigned grid = static_cast<unsigned>(std::min(a.first[a.count], MAX_GRID));
     if (bits == 32)
@@ -511,7 +519,7 @@ hipError_t launch_adamw(const moe_param* params, int count, int bits, const moe_
 hipError_t launch_adamw_states(const moe_param* params, int count, float* const* m, float* const* v,
                                hipStream_t s) {
   prof_begin(K_ADAMW_STATES, s);
-  const bool any = in_launches(params, count, PIECE, [&](Tensors& a, int first) {
+  const bool any = in_launches(params, count, 1024 * GROUPS_READ, [&](Tensors& a, int first) {
     for (int j = 0; j < a.count; ++j) {
       a.p[j].w = m[first + j];
       a.p[j].w_copy = reinterpret_cast<uint16_t*>(v[first + j]);
