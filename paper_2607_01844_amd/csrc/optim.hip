@@ -147,22 +147,22 @@ __device__ __forceinline__ float decode(uint32_t code, uint32_t scale) {
   const float mag = __uint_as_float((c << 20) + (scale << 23)) - u;
   return SIGNED && (code & 128u) ? -mag : mag;
 }
-// The exponent of u for a block whose largest magnitude has the bits `top`; 255
-// (every value NaN) where it is not finite.
+// The exponent of u for a block whose largest magnitude has the bits `top` (of v', which
+// is not below 0, with the sign bit a NaN may have); 255 (every value NaN) where it is
+// not finite.
 template <bool SIGNED>
 __device__ __forceinline__ uint32_t scale_of(uint32_t top) {
   const int e = static_cast<int>(top >> 23);
-  return e == 255 ? 255u : static_cast<uint32_t>(max(e - (SIGNED ? M_SPAN : V_SPAN), 1));
+  return e >= 255 ? 255u : static_cast<uint32_t>(max(e - (SIGNED ? M_SPAN : V_SPAN), 1));
 }
+// r: 16 random bits at place 4, and a half below them (bit 3).  Codes of a block with
+// scale 255 are not used.
 template <bool SIGNED>
-__device__ __forceinline__ uint32_t encode(float x, uint32_t scale, uint32_t r16) {
+__device__ __forceinline__ uint32_t encode(float x, uint32_t scale, uint32_t r) {
   const float u = __uint_as_float(scale << 23);
-  uint32_t c = ((__float_as_uint(fabsf(x) + u) + (r16 << 4) + 8u) >> 20) - (scale << 3);
-  if (SIGNED)
-    c |= __float_as_uint(x) >> 31 << 7;
-  else
-    c = max(c, x > 0.0f ? 1u : 0u);
-  return scale == 255u ? 0u : c;
+  const uint32_t c = ((__float_as_uint(fabsf(x) + u) + r) >> 20) - (scale << 3);
+  if (SIGNED) return c | (__float_as_uint(x) >> 24 & 128u);
+  return max(c, min(__float_as_uint(x), 1u));
 }
 
 // ------------------------------------------------------------------- AdamW
@@ -251,7 +251,7 @@ __device__ __forceinline__ void adamw_piece(const moe_param& p, int64_t base, co
       m[u][k] = st.b1 * m[u][k] + st.a1 * x;
       v[u][k] = st.b2 * v[u][k] + st.a2 * (x * x);
       top_m = max(top_m, __float_as_uint(m[u][k]) & 0x7fffffffu);
-      top_v = max(top_v, __float_as_uint(v[u][k]) & 0x7fffffffu);
+      top_v = max(top_v, __float_as_uint(v[u][k]));
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -271,9 +271,11 @@ __device__ __forceinline__ void adamw_piece(const moe_param& p, int64_t base, co
       uint32_t cm = 0, cv = 0;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        cm |= encode<true>(m[u][k], sm, r[k] & 0xffffu) << (8 * k);
-        cv |= encode<false>(v[u][k], sv, r[k] >> 16) << (8 * k);
+        cm |= encode<true>(m[u][k], sm, (r[k] << 4 & 0xffff0u) | 8u) << (8 * k);
+        cv |= encode<false>(v[u][k], sv, (r[k] >> 12 & 0xffff0u) | 8u) << (8 * k);
       }
+      if (sm == 255u) cm = 0;
+      if (sv == 255u) cv = 0;
       store4b(static_cast<uint8_t*>(p.m), i, in[u], cm);
       store4b(static_cast<uint8_t*>(p.v), i, in[u], cv);
       if ((threadIdx.x & 31) == 0 && in[u] > 0) {
@@ -292,8 +294,8 @@ __device__ __forceinline__ void adamw_piece(const moe_param& p, int64_t base, co
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t x = __float_as_uint(w[u][k]);
-        b[k] = (x & 0x7f800000u) == 0x7f800000u ? x | ((x & 0x7fffffu) ? 0x400000u : 0u)
-                                               : x + (r[k] * 0xBB67AE85u >> 16);
+        // (an infinity stays one; a NaN is left as it is, or it could wrap to a number)
+        b[k] = w[u][k] != w[u][k] ? x | 0x400000u : x + (r[k] * 0xBB67AE85u >> 16);
       }
       store4h(static_cast<uint16_t*>(p.w), i, in[u], b[0] >> 16 | (b[1] & 0xffff0000u),
               b[2] >> 16 | (b[3] & 0xffff0000u));
