@@ -535,7 +535,7 @@ int moe_vocab_distill_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_
  * ids [N] int32; w, dw [rows][H] bf16; y, dy [N][H] bf16.  Limits: 0 <= N < 2^26,
  * 1 <= rows < 2^28, begin + rows <= 2^31, N * H < 2^38, scale finite.  Workspace
  * (none for N = 0): the sorted tokens and fp32 sums of runs cut at every 8 to 64
- * sorted tokens, at most N H bytes and 24 N, and 1 MiB.
+ * sorted tokens, at most (N + 7) H bytes and 24 N, and 1 MiB.
  */
 int moe_embedding_fwd(const int32_t* ids, const moe_bf16* w, int64_t N, int H, int64_t begin,
                       int64_t rows, float scale, moe_bf16* y, void* stream);

@@ -189,6 +189,7 @@ __host__ __device__ inline double power(double b, uint32_t t) {
 }
 __host__ __device__ inline Step step_numbers(double lr, double b1, double b2, double eps, double wd,
                                              uint32_t t) {
+#pragma clang fp contract(off)  // the device's numbers are the host's
   Step s;
   s.b1 = static_cast<float>(b1);
   s.a1 = static_cast<float>(1.0 - b1);

@@ -130,10 +130,10 @@ def test_workspaces(lib):
     def query(name, *a):
         n = ctypes.c_size_t()
         return getattr(lib, name)(*a, ctypes.byref(n)), n.value
-    for N, H, rows in ((1, 8, 1), (8192, 128, 1000), (8193, 4096, 200000), (65536, 4096, 200000),
+    for N, H, rows in ((1, 8, 1), (1, 262144, 9), (9, 262144, 1 << 20), (8192, 128, 1000), (8193, 4096, 200000), (65536, 4096, 200000),
                        ((1 << 26) - 1, 2048, (1 << 28) - 1)):
         rc, n = query("moe_embedding_bwd_workspace_bytes", N, H, rows)
-        assert rc == 0 and 0 < n <= N * H + 24 * N + (8 * H) + (1 << 20), (N, H, rows, n)
+        assert rc == 0 and 0 < n <= (N + 7) * H + 24 * N + (1 << 20), (N, H, rows, n)
         assert ebwd(N=N, H=H, rows=rows, nws=n - 1)(lib) == -3
         assert ebwd(N=N, H=H, rows=rows, ws=Z)(lib) == -3
     for T, d in ((1, 8), (65536, 4096), (5, 262144), ((1 << 31) - 1, 64)):
