@@ -20,7 +20,7 @@ namespace {
 
 constexpr int SORT_W = 16;        // waves of a sorting workgroup
 constexpr int SORT_SMALL = 8192;  // tokens that one workgroup sorts
-constexpr int SORT_BITS = 9;      // widest digit
+constexpr int SORT_BITS = 10;     // widest digit: two of them sort up to 2^20 - 1 rows
 constexpr int SORT_BLOCKS = 64;   // workgroups of a sorting pass, up to 2^20 tokens
 constexpr int ZERO_ROWS = 32;     // rows looked up by a workgroup
 
@@ -92,8 +92,8 @@ __device__ __forceinline__ int lower_lanes(uint64_t m, int lane) {
   return __popcll(m & (lane == 0 ? 0ull : (~0ull >> (64 - lane))));
 }
 
-// Exclusive sums over `bins` <= 512 values, one a thread of the workgroup's first
-// `bins` (v = 0 beyond): every thread calls it.
+// Exclusive sums over at most 1024 values, one a thread of the workgroup's first (v = 0
+// beyond): every thread calls it.
 __device__ __forceinline__ int scan_bins(int v, int* wsum) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   int incl = v;

@@ -913,7 +913,8 @@ def moe_adamw_step(params, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_dec
     first) are numbers, or device tensors [1] (fp32, int32) that a captured step
     reads at every replay.  grad_sumsq [1] fp32: gradients are clipped to a norm of
     max_norm by it, and a step with a sum that is not finite is left out.  seed: of
-    the random rounding of 8-bit states and of bf16 weights (with the step)."""
+    the random rounding of 8-bit states and of bf16 weights (with the step and the
+    tensor's place in the list; give lists of one model seeds of their own)."""
     params.on_device()
     if params.w is None:
         raise ValueError("these params have no weights")
