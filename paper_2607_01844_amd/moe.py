@@ -652,13 +652,13 @@ def moe_vocab_distill_bwd(x, w_voc, topk_idx, topk_logit, lse, y_topk, dloss, vb
 
 
 # --------------------------------------------------------------- embedding
-def _given_2d(t, name):
-    """(rows, columns) of a bf16 matrix on the current device."""
-    if (t is not None and t.dtype is torch.bfloat16 and t.is_cuda and t.dim() == 2 and
+def _shape(t, dtype, name, dim):
+    """The shape of a tensor argument of this type and rank on the current device."""
+    if (t is not None and t.dtype is dtype and t.is_cuda and t.dim() == dim and
             t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice()):
         return t.shape
-    _need(t, torch.bfloat16, name, 2)
-    return _given(t, torch.bfloat16, name, t.shape).shape
+    _need(t, dtype, name, dim)
+    return _given(t, dtype, name, t.shape).shape
 
 
 def _like(t, like, name):
@@ -672,9 +672,8 @@ def moe_embedding_fwd(ids, w, scale=1.0, vocab_begin=0, y=None):
     """Rows of w [rows,H] bf16 (vocabulary entries [vocab_begin, vocab_begin +
     rows)) for ids [N] int32, times scale; zeros for ids outside them (another
     rank's, or -1 for padding).  Returns y [N,H] bf16."""
-    rows, H = _given_2d(w, "w")
-    _need(ids, torch.int32, "ids", 1)
-    N = _given(ids, torch.int32, "ids", ids.shape).shape[0]
+    rows, H = _shape(w, torch.bfloat16, "w", 2)
+    N, = _shape(ids, torch.int32, "ids", 1)
     y = w.new_empty((N, H)) if y is None else _given(y, torch.bfloat16, "y", (N, H))
     _check(lib.moe_embedding_fwd(ids.data_ptr(), w.data_ptr(), N, H, vocab_begin, rows, scale,
                                  y.data_ptr(), _stream()), "moe_embedding_fwd")
@@ -684,7 +683,7 @@ def moe_embedding_fwd(ids, w, scale=1.0, vocab_begin=0, y=None):
 def moe_embedding_bwd(ids, dy, rows, scale=1.0, vocab_begin=0, dw=None):
     """Gradient of the embedding's weights from dy [N,H] bf16: dw [rows,H] bf16,
     every row written (zeros where no token named it)."""
-    N, H = _given_2d(dy, "dy")
+    N, H = _shape(dy, torch.bfloat16, "dy", 2)
     _given(ids, torch.int32, "ids", (N,))
     ws = workspace(_ws_bytes("moe_embedding_bwd_workspace_bytes", N, H, rows), dy.device,
                    "embedding_bwd")
@@ -700,7 +699,7 @@ def moe_layer_norm_fwd(x, gamma, beta=None, eps=1e-5, residual=None, y=None, h=N
     """Layer norm of h = x + residual (rounded to bf16; h is x without a
     residual), rows [T,d] bf16, gamma and beta [d] fp32.  Returns (y, h, mean
     [T], rstd [T]); stats=False: None in the place of the last two."""
-    T, d = shape = _given_2d(x, "x")
+    T, d = shape = _shape(x, torch.bfloat16, "x", 2)
     _given(gamma, torch.float32, "gamma", (d,))
     if beta is not None:
         _given(beta, torch.float32, "beta", (d,))
@@ -724,7 +723,7 @@ def moe_layer_norm_bwd(dy, h, gamma, mean, rstd, dh=None, dx=None, with_dbeta=Tr
     rstd; dh [T,d]: the gradient that reaches h by another way (the residual
     stream's), added to dx.  Returns (dx [T,d] bf16, dgamma [d], dbeta [d] or
     None, fp32); dx is the gradient of x and of the residual alike."""
-    T, d = shape = _given_2d(h, "h")
+    T, d = shape = _shape(h, torch.bfloat16, "h", 2)
     _given(dy, torch.bfloat16, "dy", shape)
     _given(gamma, torch.float32, "gamma", (d,))
     _given(mean, torch.float32, "mean", (T,))
@@ -918,6 +917,8 @@ def moe_adamw_step(params, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_dec
     params.on_device()
     if params.w is None:
         raise ValueError("these params have no weights")
+    if not params.count:
+        return
     if grad_sumsq is not None:
         _given(grad_sumsq, torch.float32, "grad_sumsq", (1,))
     lr, lr_device = _number(lr, torch.float32, "lr")
@@ -934,6 +935,8 @@ def moe_adamw_states(params, m=None, v=None):
     params.on_device()
     if params.w is None or params.bits != 8:
         raise ValueError("these params have no 8-bit states")
+    if not params.count:
+        return [], []
     out = []
     for name, given in (("m", m), ("v", v)):
         given = [None] * params.count if given is None else list(given)

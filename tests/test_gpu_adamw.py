@@ -227,6 +227,18 @@ def test_special_gradients_without_a_norm():
         assert w[300] and w[700] and int(w.sum()) == 2
 
 
+def test_empty_lists():
+    from paper_2607_01844_amd import moe
+    for bits in (8, 32):
+        p = moe.Params([], [], bits=bits)
+        moe.moe_adamw_step(p, 1e-3, 1)
+        assert float(moe.moe_grad_sumsq(p)) == 0
+    assert moe.moe_adamw_states(moe.Params([], [], bits=8)) == ([], [])
+    none = moe.Params([torch.zeros(0, device="cuda")], [torch.zeros(0, device="cuda")], bits=8)
+    moe.moe_adamw_step(none, 1e-3, 1)
+    assert moe.moe_adamw_states(none)[0][0].numel() == 0
+
+
 def test_rows_behind_a_tensor_are_left():
     from paper_2607_01844_amd import moe
     n, room = 1001, 1408
