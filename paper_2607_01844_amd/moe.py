@@ -852,7 +852,8 @@ class Params:
         return t.data_ptr(), _TYPES.get(t.dtype, 0)
 
     def set_grads(self, g):
-        """Other gradient tensors, one for each weight."""
+        """Other gradient tensors, one for each weight.  (A captured step reads those it
+        was captured with: keep them.)"""
         g = list(g)
         if len(g) != self.count:
             raise ValueError("g needs one entry for each tensor")
