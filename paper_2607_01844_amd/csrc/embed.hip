@@ -78,15 +78,18 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const int32_t* __restric
 }
 
 // ------------------------------------------------------------------ sorting
-// The lanes of a wave whose digit (nbits of it) equals this one's.
+// The lanes of a wave that have this lane's digit (nbits of it).  Four vector
+// instructions a bit: they bound the sort of one workgroup.
 __device__ __forceinline__ uint64_t same_digit(uint32_t digit, int nbits, bool in) {
-  uint64_t same = __ballot(in);
+  const uint64_t all = __ballot(in);
+  uint32_t lo = static_cast<uint32_t>(all), hi = static_cast<uint32_t>(all >> 32);
   for (int b = 0; b < nbits; ++b) {
-    const bool bit = (digit >> b) & 1;
-    const uint64_t bal = __ballot(bit);
-    same &= bit ? bal : ~bal;
+    const uint32_t mine = static_cast<uint32_t>(__builtin_amdgcn_sbfe(static_cast<int>(digit), b, 1));
+    const uint64_t bal = __ballot(mine != 0);
+    lo &= ~(static_cast<uint32_t>(bal) ^ mine);
+    hi &= ~(static_cast<uint32_t>(bal >> 32) ^ mine);
   }
-  return same;
+  return static_cast<uint64_t>(hi) << 32 | lo;
 }
 __device__ __forceinline__ int lower_lanes(uint64_t m, int lane) {
   return __popcll(m & (lane == 0 ? 0ull : (~0ull >> (64 - lane))));
@@ -107,6 +110,25 @@ __device__ __forceinline__ int scan_bins(int v, int* wsum) {
   int base = 0;
   for (int i = 0; i < w; ++i) base += wsum[i];
   return base + incl - v;
+}
+
+// A digit's counts of the workgroup's waves, all read before any is overwritten (one
+// by one, each load would wait for the store before it), and their sum; then the
+// waves' first places, from `first` on.
+__device__ __forceinline__ int wave_counts(int (&c)[SORT_W], const int* cnt, int bins) {
+  int sum = 0;
+#pragma unroll
+  for (int u = 0; u < SORT_W; ++u) c[u] = cnt[u * bins];
+#pragma unroll
+  for (int u = 0; u < SORT_W; ++u) sum += c[u];
+  return sum;
+}
+__device__ __forceinline__ void wave_places(const int (&c)[SORT_W], int* cnt, int bins, int first) {
+#pragma unroll
+  for (int u = 0; u < SORT_W; ++u) {
+    cnt[u * bins] = first;
+    first += c[u];
+  }
 }
 
 // Up to SORT_SMALL tokens in one workgroup: every pass ranks the tokens of each
@@ -151,16 +173,10 @@ __global__ __launch_bounds__(64 * SORT_W) void embed_sort_small_kernel(
       }
     }
     __syncthreads();
-    int run = 0;
-    if (tid < bins)
-      for (int u = 0; u < SORT_W; ++u) {
-        const int c = cnt[u * bins + tid];
-        cnt[u * bins + tid] = run;
-        run += c;
-      }
-    const int first = scan_bins(tid < bins ? run : 0, wsum);
-    if (tid < bins)
-      for (int u = 0; u < SORT_W; ++u) cnt[u * bins + tid] += first;
+    int c[SORT_W], run = 0;
+    if (tid < bins) run = wave_counts(c, cnt + tid, bins);
+    const int first = scan_bins(run, wsum);
+    if (tid < bins) wave_places(c, cnt + tid, bins, first);
     __syncthreads();
 #pragma unroll
     for (int it = 0; it < R; ++it)
@@ -238,12 +254,9 @@ __global__ __launch_bounds__(64 * SORT_W) void embed_place_kernel(
   }
   const int first = scan_bins(total, wsum) + before;  // its barrier: the counts are whole
   if (tid < bins) {
-    int run = first;
-    for (int u = 0; u < SORT_W; ++u) {
-      const int c = cnt[u * bins + tid];
-      cnt[u * bins + tid] = run;
-      run += c;
-    }
+    int c[SORT_W];
+    wave_counts(c, cnt + tid, bins);
+    wave_places(c, cnt + tid, bins, first);
   }
   __syncthreads();
   for (int64_t a0 = base; a0 < end; a0 += 64) {

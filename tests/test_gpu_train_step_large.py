@@ -12,9 +12,6 @@ pytestmark = pytest.mark.gpu
 @pytest.fixture(autouse=True)
 def free_after():
     yield
-    from paper_2607_01844_amd import moe
-    moe._ws_cache.clear()
-    moe._ws_retired.clear()
     torch.cuda.empty_cache()
 
 
