@@ -10,7 +10,7 @@
 // the HBM stream of their rows, the gradient mostly by writing dW.  65536 tokens,
 // H = 4096: the forward 128 us (5.7 TB/s of rows read and written), sorting 25, sums
 // and zeros of 200,000 rows 405 (5.4 TB/s; 2000 rows: 104), joining 15; with few
-// tokens the launches and their latency (256 tokens, H = 128: 3, then 7, 5 and 3).
+// tokens the launches and their latency (256 tokens, H = 128: 3, then 5, 5 and 3).
 #include <algorithm>
 
 #include "common.h"
