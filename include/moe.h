@@ -621,14 +621,16 @@ int moe_grad_sumsq(const moe_param* params, int count, float* sumsq, void* works
  * u (2^k (1 + j / 8) - 1); m has a sign in bit 7 and 7 bits of code, v 8 bits of
  * code.  The update uses m' and v' unrounded; to be held, |x| + u is rounded up or
  * down to a code with the probability that makes the mean right, and v' > 0 has
- * code 1 at least.  m' and v' are formed without fused operations, and the 16 random
- * bits of an element are fixed (all in 32-bit integers that wrap):
+ * code 1 at least.  No code passes 8 (255 - s) - 1, the last that stands for a finite
+ * value (s of 240 for m and 224 for v reach it: values above 1.875 2^127 go down to
+ * it).  m' and v' are formed without fused operations, and the 16 random bits of an
+ * element are fixed (all in 32-bit integers that wrap):
  *   mix(x, q): x ^= x >> 16; x *= q; x ^= x >> 15
  *   key = mix(mix(seed + 0x85A308D3 t + 0x9E3779B9 j, 0x6A09E667), 0xBB67AE85),
  *         j the tensor's place in the list
  *   r = mix(0x9E3779B9 i + key, 0x6A09E667), i the element's place in its tensor;
  *   the low half of r is m's, the high half v's;
- *   code = (bits(|x| + u) + 16 r16 + 8) >> 20, less 8 s
+ *   code = (bits(|x| + u) + 16 r16 + 8) >> 20, less 8 s, within the ends above
  * so codes are a function of the inputs, bit for bit.  (For gradients of N(0, 1) an
  * element's update is off by 10 % at beta2 = 0.95 and 13 % at 0.999 in the root mean
  * square, without bias.)  bf16 weights (with either

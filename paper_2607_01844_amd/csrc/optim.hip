@@ -15,8 +15,8 @@
 // the first three bits of mantissa of |x| + u, counted from u: segments of eight
 // equal steps, each segment twice as wide as the one before (as telephony compands
 // speech), the first ending at u.  What is cut off is rounded up or down at random
-// with the right mean: v moves by a few percent a step or less, which the nearest of
-// steps of 1/8 would never follow.  A v above 0 is never held as 0, so that m / sqrt(v)
+// with the right mean (at fp32's end, above 1.875 * 2^127, down): v moves by a few
+// percent a step or less, which the nearest of steps of 1/8 would never follow.  A v above 0 is never held as 0, so that m / sqrt(v)
 // stays bounded where v is small beside its block.  m', v' are formed in fp32 without
 // contraction, so that codes are a function of the inputs alone.
 #include <algorithm>
@@ -164,6 +164,21 @@ __device__ __forceinline__ uint32_t encode(float x, uint32_t scale, uint32_t r) 
   if (SIGNED) return c | (__float_as_uint(x) >> 24 & 128u);
   return max(c, min(__float_as_uint(x), 1u));
 }
+// Four codes of a block with one of the last scales (the largest value in fp32's last
+// octave, or not finite): at most the last code that stands for a finite value, else
+// 1.875 * 2^127 and what lies above it could round up to the code of 2^128, an infinity.
+// Other blocks' codes stay below by themselves, so none of them is compared: the scale is.
+template <bool SIGNED>
+__device__ __forceinline__ uint32_t last_codes(uint32_t codes, uint32_t scale) {
+  if (scale == 255u) return 0u;
+  const uint32_t most = 8u * (255u - scale) - 1u;
+  uint32_t out = 0;
+  for (int k = 0; k < 32; k += 8) {
+    const uint32_t c = codes >> k & 255u, sign = SIGNED ? c & 128u : 0u;
+    out |= (min(c - sign, most) | sign) << k;
+  }
+  return out;
+}
 
 // ------------------------------------------------------------------- AdamW
 // The root within a unit in the last place; the instruction takes values below the
@@ -275,8 +290,8 @@ __device__ __forceinline__ void adamw_piece(const moe_param& p, int64_t base, co
         cm |= encode<true>(m[u][k], sm, (r[k] << 4 & 0xffff0u) | 8u) << (8 * k);
         cv |= encode<false>(v[u][k], sv, (r[k] >> 12 & 0xffff0u) | 8u) << (8 * k);
       }
-      if (sm == 255u) cm = 0;
-      if (sv == 255u) cv = 0;
+      if (sm >= 254u - M_SPAN) cm = last_codes<true>(cm, sm);
+      if (sv >= 254u - V_SPAN) cv = last_codes<false>(cv, sv);
       store4b(static_cast<uint8_t*>(p.m), i, in[u], cm);
       store4b(static_cast<uint8_t*>(p.v), i, in[u], cv);
       if ((threadIdx.x & 31) == 0 && in[u] > 0) {
