@@ -27,9 +27,9 @@
  *    on the host before any HIP call; on MOE_ERR_INVALID_ARG or
  *    MOE_ERR_WORKSPACE nothing was enqueued and outputs are untouched.
  *    moe_last_error() returns a message for the calling thread's last error.
- *  - Outputs must not alias inputs (moe_route_bwd's dx, updated in place, is
- *    the one exception).  Results are bitwise deterministic run to run (no
- *    floating-point atomics).
+ *  - Outputs must not alias inputs (but for moe_route_bwd's dx, updated in
+ *    place, and moe_layer_norm_bwd's).  Results are bitwise deterministic run
+ *    to run (no floating-point atomics).
  *  - cap >= T * min(k, num_local) is the row capacity of permuted buffers;
  *    rows [M, cap) of them are never read and are left unspecified.
  *  - Limits: 1 <= k <= MOE_MAX_K, k <= E <= MOE_MAX_E, T >= 0,
@@ -123,8 +123,8 @@ int moe_route(const moe_bf16* x, const float* w_router, const float* router_bias
  * and dbias are fp32 in both.
  * dx_accumulate = 1 adds the router's share to the expert path's input
  * gradient already in dx (e.g. from the unit-weight moe_combine of dx_perm),
- * giving the whole layer's dx; dx is then read and written in place (the one
- * allowed alias).  dx_accumulate = 0 writes the router's share alone.
+ * giving the whole layer's dx; dx is then read and written in place (the
+ * call's one allowed alias).  dx_accumulate = 0 writes the router's share alone.
  *
  * x [T][d] bf16; w_router [d][E] fp32; logits [T][E] fp32 (as moe_route
  * wrote them); topk_idx, topk_gate, dgate [T][k]; dw_router [d][E] fp32;
@@ -552,7 +552,7 @@ int moe_embedding_bwd(const int32_t* ids, const moe_bf16* dy, int64_t N, int H, 
  * and, given dy = dL/dy and dh = dL/dh of what else reads h (NULL: nothing), with
  * xh_j = (h_j - mean) rstd and g_j = dy_j gamma_j:
  *   dx_j = bf16(dh_j + rstd (g_j - sum g / d - xh_j sum(g xh) / d))
- *          (the gradient of x and of residual alike)
+ *          (the gradient of x and of residual alike; dx may be dy, h or dh itself)
  *   dgamma_j = sum over rows of dy_j xh_j, dbeta_j = sum over rows of dy_j
  * Statistics and sums are fp32 in a fixed order.  x, residual, h, y, dy, dh, dx
  * [T][d] bf16; gamma, beta, dgamma, dbeta [d] fp32; mean, rstd [T] fp32 (NULL in

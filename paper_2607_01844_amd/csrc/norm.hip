@@ -167,13 +167,14 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_fwd_kernel(
   }
 }
 
-// part [workgroups][2][d]: the workgroup's sums of dy xh and of dy.
+// part [workgroups][2][d]: the workgroup's sums of dy xh and of dy.  dx may lie in the
+// memory of dy, h or dh (so these promise nothing of each other): every thread reads
+// what it overwrites before, and nothing else is read there.
 template <int W, int C, bool DH, bool STREAM>
 __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_bwd_kernel(
-    const uint16_t* __restrict__ dy, const uint16_t* __restrict__ h,
-    const float* __restrict__ gamma, const float* __restrict__ mean,
-    const float* __restrict__ rstd, const uint16_t* __restrict__ dh, int64_t T, int d,
-    uint16_t* __restrict__ dx, float* __restrict__ part) {
+    const uint16_t* dy, const uint16_t* h, const float* __restrict__ gamma,
+    const float* __restrict__ mean, const float* __restrict__ rstd, const uint16_t* dh, int64_t T,
+    int d, uint16_t* dx, float* __restrict__ part) {
   constexpr int G = W < 4 ? 4 / W : 1, R = 1;
   __shared__ float red[2][2 * R * W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -353,10 +354,9 @@ __global__ __launch_bounds__(1024) void norm_fwd_long_kernel(
 
 template <bool DH>
 __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(
-    const uint16_t* __restrict__ dy, const uint16_t* __restrict__ h,
-    const float* __restrict__ gamma, const float* __restrict__ mean,
-    const float* __restrict__ rstd, const uint16_t* __restrict__ dh, int64_t T, int d,
-    uint16_t* __restrict__ dx) {
+    const uint16_t* dy, const uint16_t* h, const float* __restrict__ gamma,
+    const float* __restrict__ mean, const float* __restrict__ rstd, const uint16_t* dh, int64_t T,
+    int d, uint16_t* dx) {
   __shared__ float red[2][32];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nch = d >> 3;
   const float fd = static_cast<float>(d);
@@ -546,13 +546,14 @@ hipError_t launch_norm_bwd(const uint16_t* dy, const uint16_t* h, const float* g
   if (T > 0) {
     prof_begin(K_NORM_BWD, s);
     if (d > NORM_HELD) {
+      // the columns' sums first: dx may lie in the memory of dy or h
+      const dim3 cols(static_cast<unsigned>(ceil_div(d, 2048)), static_cast<unsigned>(groups));
+      norm_cols_kernel<<<cols, 256, 0, s>>>(dy, h, mean, rstd, T, d, ceil_div(T, groups), part);
       const unsigned grid = static_cast<unsigned>(std::min<int64_t>(T, 2 * device_cus()));
       if (dh)
         norm_bwd_long_kernel<true><<<grid, 1024, 0, s>>>(dy, h, gamma, mean, rstd, dh, T, d, dx);
       else
         norm_bwd_long_kernel<false><<<grid, 1024, 0, s>>>(dy, h, gamma, mean, rstd, dh, T, d, dx);
-      const dim3 cols(static_cast<unsigned>(ceil_div(d, 2048)), static_cast<unsigned>(groups));
-      norm_cols_kernel<<<cols, 256, 0, s>>>(dy, h, mean, rstd, T, d, ceil_div(T, groups), part);
     } else {
       const bool stream = T * d * (dh ? 8 : 6) >= STREAM_BWD;
       by_width(d, [&](auto w, auto c) {

@@ -722,7 +722,8 @@ def moe_layer_norm_bwd(dy, h, gamma, mean, rstd, dh=None, dx=None, with_dbeta=Tr
     """Gradients of the layer norm from dy [T,d] and the forward's h, mean and
     rstd; dh [T,d]: the gradient that reaches h by another way (the residual
     stream's), added to dx.  Returns (dx [T,d] bf16, dgamma [d], dbeta [d] or
-    None, fp32); dx is the gradient of x and of the residual alike."""
+    None, fp32); dx is the gradient of x and of the residual alike, and may be dy, h
+    or dh itself."""
     T, d = shape = _shape(h, torch.bfloat16, "h", 2)
     _given(dy, torch.bfloat16, "dy", shape)
     _given(gamma, torch.float32, "gamma", (d,))
