@@ -747,11 +747,29 @@ _TYPES = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}
 STATE_BLOCK = 128  # elements of one scale of an 8-bit state
 
 
+def _same_order(a, b):
+    """Whether two shapes of as many elements name them in one order: the places where
+    the axes of one end are among those of the other (neighbouring axes are taken
+    together, all of them in a flat tensor; axes of 1 aside)."""
+    if a == b or 0 in a:
+        return True
+    ends = []
+    for shape in (a, b):
+        n, at = 1, set()
+        for size in shape:
+            n *= size
+            at.add(n)
+        ends.append(at - {1, n})
+    return ends[0] <= ends[1] or ends[1] <= ends[0]
+
+
 class Params:
     """The tensors of a weight update, checked once and kept: weights w (fp32 or
     bf16), gradients g (fp32 or bf16), states m and v, and optionally bf16 copies
     of fp32 weights that each step writes (w_copy; None where a weight has none).
-    Lists of the same length; tensors of any shape, contiguous, of equal sizes.
+    Lists of the same length; tensors of any shape, contiguous, those of one weight in
+    its order of elements: its shape, or one with neighbouring axes taken together, as
+    in a flat one ([n], or [E d, f] for [E, d, f]; a transposed gradient is refused).
     A state is an fp32 tensor, or in 8 bits a pair (codes [n] uint8, scales
     [ceil(n / 128)] uint8); without m and v they start as zeros, in `bits` bits.
     w=None: gradients alone, for moe_grad_sumsq.  The tensors stay alive as long as
@@ -771,6 +789,8 @@ class Params:
             if not isinstance(t, torch.Tensor):
                 raise ValueError(f"{name}[{i}] is required")
         sizes = [t.numel() for t in sized]
+        # the sum of squares of gradients alone goes by no order
+        self.shapes = [None if w is None else tuple(t.shape) for t in sized]
         spans = []
         if w is None:
             if m is not None or v is not None or w_copy is not None or bits is not None:
@@ -784,20 +804,20 @@ class Params:
                 self._new_states(sizes, 32 if bits is None else bits)
             else:
                 self._given_states(m, v, bits)
-            for i, (p, n) in enumerate(zip(self.array, sizes)):
+            for i, (p, n, like) in enumerate(zip(self.array, sizes, self.shapes)):
                 p.w, p.w_type = self._take(self.w[i], tuple(_TYPES), f"w[{i}]", n, spans)
                 if self.w_copy[i] is not None:
                     if p.w_type != MOE_F32:
                         raise TypeError(f"w_copy[{i}]: only fp32 weights have a copy")
                     p.w_copy, _ = self._take(self.w_copy[i], (torch.bfloat16,), f"w_copy[{i}]", n,
-                                             spans)
+                                             spans, like)
                 for name, state in (("m", self.m[i]), ("v", self.v[i])):
                     at = f"{name}[{i}]"
                     if self.bits == 32:
-                        a, _ = self._take(state, (torch.float32,), at, n, spans)
+                        a, _ = self._take(state, (torch.float32,), at, n, spans, like)
                     else:
                         codes, scales = state
-                        a, _ = self._take(codes, (torch.uint8,), at, n, spans)
+                        a, _ = self._take(codes, (torch.uint8,), at, n, spans, like)
                         b, _ = self._take(scales, (torch.uint8,), at + " scales",
                                           -(-n // STATE_BLOCK), spans)
                         setattr(p, name + "_scale", b)
@@ -832,8 +852,9 @@ class Params:
             raise ValueError(f"states are in {held} bits, not in {bits}")
         self.bits = held
 
-    def _take(self, t, dtypes, name, n, spans):
-        """(address, type) of a tensor of n elements; its span joins `spans`."""
+    def _take(self, t, dtypes, name, n, spans, like=None):
+        """(address, type) of a tensor of n elements, in the order of a tensor of shape
+        `like` (None: any); its span joins `spans`."""
         if not isinstance(t, torch.Tensor):
             raise ValueError(f"{name} is required")
         if t.dtype not in dtypes:
@@ -844,6 +865,9 @@ class Params:
             raise ValueError(f"{name} must be contiguous")
         if t.numel() != n:
             raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
+        if like is not None and t.shape != like and not _same_order(tuple(t.shape), like):
+            raise ValueError(f"{name}: shape {tuple(t.shape)} is in another order than the "
+                             f"weight's {like}")
         if self.device is None:
             self.device, self.torch_device = t.get_device(), t.device
         if t.get_device() != self.device:
@@ -859,8 +883,8 @@ class Params:
         if len(g) != self.count:
             raise ValueError("g needs one entry for each tensor")
         read = []
-        at = [self._take(t, tuple(_TYPES), f"g[{i}]", n, read)
-              for i, (t, n) in enumerate(zip(g, self.sizes))]
+        at = [self._take(t, tuple(_TYPES), f"g[{i}]", n, read, like)
+              for i, (t, n, like) in enumerate(zip(g, self.sizes, self.shapes))]
         # what a step writes lies apart from all else that it reads or writes
         spans = sorted([s + (True,) for s in self._written] + [s + (False,) for s in read])
         last, last_written = (0, 0, None), (0, 0, None)  # the spans that reach furthest
