@@ -24,17 +24,6 @@ constexpr int SORT_BITS = 10;     // widest digit: two of them sort up to 2^20 -
 constexpr int SORT_BLOCKS = 64;   // workgroups of a sorting pass, up to 2^20 tokens
 constexpr int ZERO_ROWS = 32;     // rows looked up by a workgroup
 
-__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
-  f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x);
-  f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-  f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z);
-  f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
-}
-__device__ __forceinline__ uint4 pack8(const float* f) {
-  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
-                    pack_bf16x2(f[6], f[7]));
-}
-
 // A token's row of this rank, or `rows` (none).
 __device__ __forceinline__ uint32_t row_of(int32_t id, int64_t begin, int64_t rows) {
   const int64_t v = id - begin;
