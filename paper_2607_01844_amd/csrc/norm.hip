@@ -65,8 +65,7 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_fwd_kernel(
     uint16_t* __restrict__ h, uint16_t* __restrict__ y, float* __restrict__ mean,
     float* __restrict__ rstd) {
   constexpr int G = W < 4 ? 4 / W : 1;  // rows' teams of a workgroup
-  constexpr int R = 1;                  // rows at once (2: no faster)
-  __shared__ float red[2][R * W];
+  __shared__ float red[2][W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int w = wave % W, team = wave / W;
   const int nch = d >> 3;
@@ -82,77 +81,60 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_fwd_kernel(
       if (beta) load8f(beta + 8 * at, be[c]);
     }
   }
-  const int64_t step = static_cast<int64_t>(gridDim.x) * G * R;
-  for (int64_t t0 = (static_cast<int64_t>(blockIdx.x) * G + team) * R; t0 < T; t0 += step) {
-    uint4 v[R][C], e[R][C];
+  const int64_t step = static_cast<int64_t>(gridDim.x) * G;
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * G + team; t < T; t += step) {
+    uint4 v[C], e[C];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int c = 0; c < C; ++c) {
+      const int at = (c * W + w) * 64 + lane;
+      v[c] = make_uint4(0, 0, 0, 0);
+      if (at < nch) {
+        v[c] = load_row<STREAM>(reinterpret_cast<const uint4*>(x + t * d) + at);
+        if constexpr (RES) e[c] = load_row<STREAM>(reinterpret_cast<const uint4*>(res + t * d) + at);
+      }
+    }
+    if constexpr (RES) {
 #pragma unroll
       for (int c = 0; c < C; ++c) {
         const int at = (c * W + w) * 64 + lane;
-        v[r][c] = make_uint4(0, 0, 0, 0);
-        if (at < nch && t0 + r < T) {
-          v[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(x + (t0 + r) * d) + at);
-          if constexpr (RES) e[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(res + (t0 + r) * d) + at);
+        if (at < nch) {
+          v[c] = add8(v[c], e[c]);
+          store_stream(reinterpret_cast<uint4*>(h + t * d) + at, v[c]);
         }
       }
-    if constexpr (RES) {
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int at = (c * W + w) * 64 + lane;
-          if (at < nch && t0 + r < T) {
-            v[r][c] = add8(v[r][c], e[r][c]);
-            store_stream(reinterpret_cast<uint4*>(h + (t0 + r) * d) + at, v[r][c]);
-          }
-        }
     }
-    float mu[R], sq[R];
+    float mu[1] = {0.0f}, sq[1] = {0.0f};
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      mu[r] = 0.0f;
+    for (int c = 0; c < C; ++c) {
+      float f[8];
+      unpack8(v[c], f);
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float f[8];
-        unpack8(v[r][c], f);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) mu[r] += f[q];
-      }
+      for (int q = 0; q < 8; ++q) mu[0] += f[q];
     }
     row_sums<W>(mu, red[0], w, lane);
+    mu[0] /= fd;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      mu[r] /= fd;
-      sq[r] = 0.0f;
+    for (int c = 0; c < C; ++c) {
+      float f[8];
+      unpack8(v[c], f);
+      if ((c * W + w) * 64 + lane < nch)
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float f[8];
-        unpack8(v[r][c], f);
-        if ((c * W + w) * 64 + lane < nch)
-#pragma unroll
-          for (int q = 0; q < 8; ++q) sq[r] += (f[q] - mu[r]) * (f[q] - mu[r]);
-      }
+        for (int q = 0; q < 8; ++q) sq[0] += (f[q] - mu[0]) * (f[q] - mu[0]);
     }
     row_sums<W>(sq, red[1], w, lane);
+    const float rs = 1.0f / sqrtf(sq[0] / fd + eps);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const float rs = 1.0f / sqrtf(sq[r] / fd + eps);
-      if (t0 + r < T) {
+    for (int c = 0; c < C; ++c) {
+      const int at = (c * W + w) * 64 + lane;
+      float f[8];
+      unpack8(v[c], f);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int at = (c * W + w) * 64 + lane;
-          float f[8];
-          unpack8(v[r][c], f);
-#pragma unroll
-          for (int q = 0; q < 8; ++q) f[q] = (f[q] - mu[r]) * rs * ga[c][q] + be[c][q];
-          if (at < nch) store_stream(reinterpret_cast<uint4*>(y + (t0 + r) * d) + at, pack8(f));
-        }
-        if (w == 0 && lane == 0) {
-          if (mean) mean[t0 + r] = mu[r];
-          if (rstd) rstd[t0 + r] = rs;
-        }
-      }
+      for (int q = 0; q < 8; ++q) f[q] = (f[q] - mu[0]) * rs * ga[c][q] + be[c][q];
+      if (at < nch) store_stream(reinterpret_cast<uint4*>(y + t * d) + at, pack8(f));
+    }
+    if (w == 0 && lane == 0) {
+      if (mean) mean[t] = mu[0];
+      if (rstd) rstd[t] = rs;
     }
   }
 }
@@ -165,8 +147,8 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_bwd_kernel(
     const uint16_t* dy, const uint16_t* h, const float* __restrict__ gamma,
     const float* __restrict__ mean, const float* __restrict__ rstd, const uint16_t* dh, int64_t T,
     int d, uint16_t* dx, float* __restrict__ part) {
-  constexpr int G = W < 4 ? 4 / W : 1, R = 1;
-  __shared__ float red[2][2 * R * W];
+  constexpr int G = W < 4 ? 4 / W : 1;
+  __shared__ float red[2][2 * W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int w = wave % W, team = wave / W;
   const int nch = d >> 3;
@@ -179,78 +161,62 @@ __global__ __launch_bounds__(W < 4 ? 256 : 64 * W) void norm_bwd_kernel(
     for (int q = 0; q < 8; ++q) ga[c][q] = dg[c][q] = db[c][q] = 0.0f;
     if (at < nch) load8f(gamma + 8 * at, ga[c]);
   }
-  const int64_t step = static_cast<int64_t>(gridDim.x) * G * R;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * G;
   int turn = 0;
-  for (int64_t t0 = (static_cast<int64_t>(blockIdx.x) * G + team) * R; t0 < T; t0 += step) {
-    uint4 a[R][C], b[R][C], e[R][C];
-    float mu[R], rs[R], s[2 * R];
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * G + team; t < T; t += step) {
+    uint4 a[C], b[C], e[C];
+    const float mu = mean[t], rs = rstd[t];
+    float s[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const bool in = t0 + r < T;
-      mu[r] = in ? mean[t0 + r] : 0.0f;
-      rs[r] = in ? rstd[t0 + r] : 0.0f;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int at = (c * W + w) * 64 + lane;
-        a[r][c] = b[r][c] = make_uint4(0, 0, 0, 0);
-        if (at < nch && in) {
-          a[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(dy + (t0 + r) * d) + at);
-          b[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(h + (t0 + r) * d) + at);
-          if constexpr (DH) e[r][c] = load_row<STREAM>(reinterpret_cast<const uint4*>(dh + (t0 + r) * d) + at);
-        }
+    for (int c = 0; c < C; ++c) {
+      const int at = (c * W + w) * 64 + lane;
+      a[c] = b[c] = make_uint4(0, 0, 0, 0);
+      if (at < nch) {
+        a[c] = load_row<STREAM>(reinterpret_cast<const uint4*>(dy + t * d) + at);
+        b[c] = load_row<STREAM>(reinterpret_cast<const uint4*>(h + t * d) + at);
+        if constexpr (DH) e[c] = load_row<STREAM>(reinterpret_cast<const uint4*>(dh + t * d) + at);
       }
     }
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      s[2 * r] = s[2 * r + 1] = 0.0f;
-      if (t0 + r < T) {
+    for (int c = 0; c < C; ++c) {
+      if ((c * W + w) * 64 + lane < nch) {
+        float f[8], g[8];
+        unpack8(a[c], g);
+        unpack8(b[c], f);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          if ((c * W + w) * 64 + lane < nch) {
-            float f[8], g[8];
-            unpack8(a[r][c], g);
-            unpack8(b[r][c], f);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              const float xh = (f[q] - mu[r]) * rs[r];
-              dg[c][q] += g[q] * xh;
-              db[c][q] += g[q];
-              s[2 * r] += g[q] * ga[c][q];
-              s[2 * r + 1] += g[q] * ga[c][q] * xh;
-            }
-          }
+        for (int q = 0; q < 8; ++q) {
+          const float xh = (f[q] - mu) * rs;
+          dg[c][q] += g[q] * xh;
+          db[c][q] += g[q];
+          s[0] += g[q] * ga[c][q];
+          s[1] += g[q] * ga[c][q] * xh;
         }
       }
     }
     // two places by turns: a wave may be a round ahead of another's reads
     row_sums<W>(s, red[turn], w, lane);
     turn ^= 1;
+    const float m1 = s[0] / fd, m2 = s[1] / fd;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      if (t0 + r < T) {
-        const float m1 = s[2 * r] / fd, m2 = s[2 * r + 1] / fd;
+    for (int c = 0; c < C; ++c) {
+      const int at = (c * W + w) * 64 + lane;
+      float f[8], g[8];
+      unpack8(a[c], g);
+      unpack8(b[c], f);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          const int at = (c * W + w) * 64 + lane;
-          float f[8], g[8];
-          unpack8(a[r][c], g);
-          unpack8(b[r][c], f);
+      for (int q = 0; q < 8; ++q) {
+        const float xh = (f[q] - mu) * rs;
+        f[q] = (g[q] * ga[c][q] - m1 - xh * m2) * rs;
+      }
+      if constexpr (DH) {
+        unpack8(e[c], g);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            const float xh = (f[q] - mu[r]) * rs[r];
-            f[q] = (g[q] * ga[c][q] - m1 - xh * m2) * rs[r];
-          }
-          if constexpr (DH) {
-            unpack8(e[r][c], g);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) f[q] += g[q];
-          }
-          if (at < nch) {
-            uint4* o = reinterpret_cast<uint4*>(dx + (t0 + r) * d) + at;
-            if constexpr (STREAM) store_stream(o, pack8(f));
-            else *o = pack8(f);
-          }
-        }
+        for (int q = 0; q < 8; ++q) f[q] += g[q];
+      }
+      if (at < nch) {
+        uint4* o = reinterpret_cast<uint4*>(dx + t * d) + at;
+        if constexpr (STREAM) store_stream(o, pack8(f));
+        else *o = pack8(f);
       }
     }
   }
