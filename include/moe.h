@@ -528,9 +528,9 @@ int moe_vocab_distill_bwd(const moe_bf16* x, const moe_bf16* w_voc, const int32_
  *   y[t] = bf16(scale w[ids[t] - begin]); 0 where ids[t] is outside them (another
  *          rank's, or -1 for padding), so that the ranks' outputs add up
  *   dw[v] = bf16(scale sum of dy[t] over the tokens with ids[t] = begin + v)
- * The sums are fp32 in an order that only the ids set (runs of ascending t, joined
- * in order): equal bits run to run.  Every row of dw is written, those without
- * tokens as zeros.  A NaN in dy stays in its row.
+ * The sums are fp32 in an order that the ids, N and H set (runs of ascending t, whose
+ * sums are joined in a fixed order): equal bits run to run.  Every row of dw is
+ * written, those without tokens as zeros.  A NaN in dy stays in its row.
  *
  * ids [N] int32; w, dw [rows][H] bf16; y, dy [N][H] bf16.  Limits: 0 <= N < 2^26,
  * 1 <= rows < 2^28, begin + rows <= 2^31, N * H < 2^38, scale finite.  Workspace

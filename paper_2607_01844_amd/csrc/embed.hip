@@ -5,12 +5,15 @@
 // cuts the sorted list into pieces of equal length, so that a frequent word costs
 // no wave more than a rare one: a run of one row inside a piece is summed in
 // registers and written; one that passes a piece's end leaves fp32 partial sums,
-// which are joined in order.  Rows without tokens are written as zeros by
-// workgroups that look them up in the sorted list.  Both directions are bound by
-// the HBM stream of their rows, the gradient mostly by writing dW.  65536 tokens,
-// H = 4096: the forward 128 us (5.7 TB/s of rows read and written), sorting 25, sums
-// and zeros of 200,000 rows 405 (5.4 TB/s; 2000 rows: 104), joining 15; with few
-// tokens the launches and their latency (256 tokens, H = 128: 3, then 5, 5 and 3).
+// which are joined in a fixed order (each team of lanes takes every so many-th, then the
+// teams are added up).  Rows without tokens are written as zeros by workgroups that look
+// them up in the sorted list.  Both directions are bound by the HBM stream of their rows,
+// the gradient mostly by writing dW.  65536 tokens by Zipf's law, H = 4096, 200,000 rows:
+// the forward 130 us (5.5 TB/s), sorting 25, sums and zeros 375 (5.8 TB/s), joining 18;
+// the forward takes 175 right after such a gradient and the gradient 30 less than
+// otherwise (its 1.6 GB are still on their way to memory when the next kernel starts);
+// 2000 rows: sums and joining 121.  With few tokens it is the launches and their
+// latency (256 tokens, H = 128: 3 us, then 5, 4 and 3).
 #include <algorithm>
 
 #include "common.h"

@@ -7,8 +7,8 @@
 // mean is subtracted before the squares are summed (a row far from zero keeps its
 // variance).  Sums, statistics and the weights' gradients are fp32; every
 // bf16 result is rounded once.  Bound by the HBM stream: T = 65536, d = 4096 with the
-// residual, 2.1 GB each way, forward 5.7 to 6 TB/s, backward 5.7 to 6.2; few rows by
-// latency (16 of them: 4 us).
+// residual, 2.15 GB each way, forward 380 us, 5.6 TB/s, backward 373, 5.75; few rows by
+// latency (16 of them: 3.4 us).
 #include <algorithm>
 
 #include "common.h"
@@ -416,11 +416,11 @@ constexpr int NORM_HELD = 16384;  // widest row held in registers
 
 // Two workgroups a compute unit walk the rows (three of narrow rows, one of 16 waves in
 // the backward pass): few rows in flight, far apart, suit HBM best (T = 65536, d = 4096,
-// 2.1 GB each way: forward 358 us on 512 workgroups, 379 on 768, 398 on 2048; backward
-// 342, 373, 394; d = 512: 39, 38 and 45, 43).
+// 2.15 GB each way: forward 424 us on 256 workgroups, 381 on 512, 388 on 768, 398 on
+// 2048; backward 431, 376, 438, 444; d = 512: 43 on 512, 42 on 768, and 46, 45).
 // A backward pass has fewer where a team would get under 16 rows: its partial sums,
-// 8 bytes a column, weigh against 6 or 8 a row's (T = 4096, d = 8192: 64 us on 256
-// workgroups, 67 on 512, 90 on 1024).
+// 8 bytes a column, weigh against 6 or 8 a row's (T = 4096, d = 8192: 63 us on 256
+// workgroups, 72 on 512, 91 on 1024).
 int64_t groups_a_cu(int d) { return d <= 1024 ? 3 : 2; }
 int64_t bwd_groups(int64_t T, int d) {
   if (T == 0) return 1;
@@ -432,9 +432,10 @@ int64_t bwd_groups(int64_t T, int d) {
 }
 
 // Calls that move this much gain from keeping their reads out of the caches (and the
-// backward's dx): forward of 2.1 GB 366 -> 358 us, backward 385 -> 342, of 470 MB
-// 104 -> 94; less may find its inputs there (forward of 268 MB 40 us, with streamed
-// loads 47; backward 48 and 49).  y and h are streamed always (268 MB: 44 -> 37 us).
+// backward's dx): forward of 2.15 GB 401 -> 381 us, backward 401 -> 376, of 470 MB
+// 94 -> 89; less may find its inputs there (forward of 470 MB 70 us, with streamed loads
+// 81, of 268 MB 42 and 48; backward of 268 MB 51 and 58).  y and h are streamed always
+// (2.15 GB: 397 -> 381 us, 268 MB: 43 to 45 -> 42).
 constexpr int64_t STREAM_FWD = int64_t{768} << 20, STREAM_BWD = int64_t{384} << 20;
 
 // A wave a row up to 2048 columns (32 registers of it a lane), then eight and sixteen.
@@ -473,7 +474,7 @@ hipError_t launch_norm_fwd(const uint16_t* x, const uint16_t* res, const float* 
     by_width(d, [&](auto w, auto c) {
       constexpr int W = w, C = c, G = W < 4 ? 4 / W : 1, threads = W < 4 ? 256 : 64 * W;
       // one load of 16 bytes a lane and row is too little in flight (T = 65536, d = 4096
-      // without the residual: 226 us, with twice the workgroups 196)
+      // without the residual: 217 us, with twice the workgroups 191)
       const int more = !res && W > 1 && C == 1 ? 2 : 1;
       const unsigned grid = static_cast<unsigned>(
           std::min<int64_t>(ceil_div(T, G), more * groups_a_cu(d) * device_cus()));

@@ -957,7 +957,7 @@ def moe_adamw_step(params, lr, step, beta1=0.9, beta2=0.95, eps=1e-8, weight_dec
 
 def moe_adamw_states(params, m=None, v=None):
     """The values of 8-bit states: two lists of fp32 tensors [n] (m, v: given ones
-    to write)."""
+    to write, apart from each other and from what `params` names)."""
     params.on_device()
     if params.w is None or params.bits != 8:
         raise ValueError("these params have no 8-bit states")
@@ -1060,8 +1060,9 @@ def layer_fwd_bwd(inp: dict, k: int, expert_begin=0, num_local=None, renorm=0,
     With inp["norm_gamma"] (and, optionally, norm_beta, norm_eps and residual) the
     layer stands in a pre-norm block: h = x + residual, y is the layer's output on
     the layer norm of h, and dy the gradient of h + y (the next norm's sum), which
-    reaches h both ways; dx is then the gradient of h, and h, dgamma and dbeta are
-    returned.  All experts have to be local: the ranks' dx would each hold dy.
+    reaches h both ways; dx is then the gradient of h (as without a norm, the router's
+    share is in it with router_loss only), and h, dgamma and dbeta are returned.  All
+    experts have to be local: the ranks' dx would each hold dy.
     """
     x = inp["x"]
     norm = None
